@@ -273,6 +273,68 @@ fedattn_status fedattn_decode_noalloc(const fedattn_shape *shape, int32_t mode,
                                       int64_t cache_stride_participant, const int32_t *kv_len,
                                       int32_t max_kv_len, void *o, float *lse, fedattn_stream stream);
 
+/* ---- queries and keys as the attention calls take them: norm per head and rotation ----------------
+ * Models with normalised queries and keys apply, between the projections and attention, to every head
+ * of every row: y_c = x_c * w_c / sqrt(mean_c x_c^2 + eps), then the rotation by the token's (global)
+ * position: channels (i, i + rot_dim/2), or (2i, 2i+1) when interleaved, i < rot_dim/2, are turned by
+ * the angle pos * inv_freq[i]; channels from rot_dim on are only normalised.  One pass, fp32
+ * arithmetic, one rounding; the angle is reduced exactly for any int32 position.
+ *   q dev, k dev: row i's heads [Hq,d] / [Hkv,d] at q + i * q_row_stride / k + i * k_row_stride
+ *     elements (multiples of 8, at least Hq*d / Hkv*d; 0 = packed): rows of a joint projection are read
+ *     where they lie.  q or k may be NULL, together with its output: the other is done alone.
+ *   q_weight, k_weight dev [d] in shape->dtype, or NULL (ones).  eps >= 0.  A row of zeros gives zeros
+ *     when eps > 0.
+ *   pos dev int32 [n_rows], any value, or NULL (= row index).  inv_freq_host host double [rot_dim/2],
+ *     finite, radians per position, read before the call returns (NULL when rot_dim == 0).
+ *     rot_dim: multiple of 8, 0 .. d.
+ *   q_out dev [n_rows,Hq,d], k_out dev [n_rows,Hkv,d], packed; each may be its own input when that is
+ *     packed too, and overlaps nothing else. */
+fedattn_status fedattn_qk_norm_rope(fedattn_ctx *ctx, const fedattn_shape *shape, int64_t n_rows,
+                                    const void *q, int64_t q_row_stride, const void *k, int64_t k_row_stride,
+                                    const void *q_weight, const void *k_weight, float eps,
+                                    const int32_t *pos, const double *inv_freq_host, int32_t rot_dim,
+                                    int32_t interleaved, void *q_out, void *k_out, fedattn_stream stream);
+
+/* ---- a cache held in 4 bits --------------------------------------------------------------------------
+ * Keys and values of n_caches caches of cap_rows rows each, head-major:
+ *   codes  dev uint8 [n_caches, Hkv, cap_rows, d/2]   channel 2c in the low half of byte c, 2c+1 in the high half
+ *   scales dev uint8 [n_caches, Hkv, cap_rows, d/32]  one per 32 channels
+ *   value = (nibble - 8) * scale,  scale = (8 + (b & 7)) * 2^((b >> 3) - 21):  4.25 bits per element.
+ * Every value is exact in bf16.  fedattn_quantize_kv takes the least scale whose sevenfold reaches the
+ * group's largest magnitude and the nearest code (ties to even) in -7..7; magnitudes beyond 107520
+ * saturate.  Needs head_dim a multiple of 32, cap_rows a multiple of 16, 16-byte aligned arrays, and
+ * n_caches * cap_rows <= 2^31 - 1.
+ *
+ * fedattn_quantize_kv    row i of k, v (dev, strides in elements as above) is written to row at[i] of the
+ *                        caches; at dev int32 [n_rows] = cache * cap_rows + row, or NULL (= i).  A negative
+ *                        entry skips the row, one beyond the caches skips it and raises FEDATTN_ERR_INDEX.
+ *                        Entries that are not negative are distinct: with one row twice the caches hold
+ *                        pieces of either.  Nothing but the named rows is written.
+ * fedattn_dequantize_kv  the values of row at[i] to row i of k, v (dev [n_rows, Hkv, d], packed); skipped
+ *                        rows keep what they hold.  For attention of many queries over such a cache: read the
+ *                        rows back and call fedattn_sync. */
+fedattn_status fedattn_quantize_kv(fedattn_ctx *ctx, const fedattn_shape *shape, int64_t n_rows,
+                                   const void *k, int64_t k_row_stride, const void *v, int64_t v_row_stride,
+                                   const int32_t *at, int64_t n_caches, int64_t cap_rows,
+                                   uint8_t *k_codes, uint8_t *k_scales, uint8_t *v_codes, uint8_t *v_scales,
+                                   fedattn_stream stream);
+fedattn_status fedattn_dequantize_kv(fedattn_ctx *ctx, const fedattn_shape *shape, int64_t n_rows,
+                                     const int32_t *at, int64_t n_caches, int64_t cap_rows,
+                                     const uint8_t *k_codes, const uint8_t *k_scales,
+                                     const uint8_t *v_codes, const uint8_t *v_scales,
+                                     void *k, void *v, fedattn_stream stream);
+
+/* fedattn_decode over such caches: LOCAL participant n reads cache n (n_participants caches), SYNC all read
+ * the one cache.  kv_len dev int32 as there (values above max_kv_len count as max_kv_len); max_kv_len <=
+ * cap_rows.  window == 0: every row; window >= 1: the last `window` rows and the first n_sink.  Rows from
+ * kv_len on may hold anything.  Uses the workspace for split-KV partials.  One launch, or two (stream, merge)
+ * when more than 8 CTAs share a cache. */
+fedattn_status fedattn_decode_quant(fedattn_ctx *ctx, const fedattn_shape *shape, int32_t mode, const void *q,
+                                    const uint8_t *k_codes, const uint8_t *k_scales,
+                                    const uint8_t *v_codes, const uint8_t *v_scales, int64_t cap_rows,
+                                    const int32_t *kv_len, int32_t max_kv_len, int32_t window, int32_t n_sink,
+                                    void *o, float *lse, fedattn_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

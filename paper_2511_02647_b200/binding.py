@@ -24,7 +24,8 @@ DECODE_LOCAL, DECODE_SYNC = 0, 1
 _SYMBOLS = ["fedattn_workspace_bytes", "fedattn_create", "fedattn_destroy", "fedattn_status_string",
             "fedattn_poll", "fedattn_launch_count", "fedattn_tensor_core_launch_count",
             "fedattn_selftest_wait_timeout", "fedattn_local", "fedattn_aggregate_kv",
-            "fedattn_sync", "fedattn_sync_remote", "fedattn_merge", "fedattn_decode", "fedattn_decode_noalloc"]
+            "fedattn_sync", "fedattn_sync_remote", "fedattn_merge", "fedattn_decode", "fedattn_decode_noalloc",
+            "fedattn_qk_norm_rope", "fedattn_quantize_kv", "fedattn_dequantize_kv", "fedattn_decode_quant"]
 
 
 class FedAttnError(RuntimeError):
@@ -112,6 +113,15 @@ def _load():
     lib.fedattn_decode.argtypes = [vp, C.POINTER(Shape), i32, vp, vp, vp, i64, vp, i32, vp, vp, vp]
     lib.fedattn_decode_noalloc.restype = C.c_int
     lib.fedattn_decode_noalloc.argtypes = [C.POINTER(Shape), i32, vp, vp, vp, i64, vp, i32, vp, vp, vp]
+    lib.fedattn_qk_norm_rope.restype = C.c_int
+    lib.fedattn_qk_norm_rope.argtypes = [vp, C.POINTER(Shape), i64, vp, i64, vp, i64, vp, vp, C.c_float, vp, vp, i32, i32, vp,
+                                         vp, vp]
+    lib.fedattn_quantize_kv.restype = C.c_int
+    lib.fedattn_quantize_kv.argtypes = [vp, C.POINTER(Shape), i64, vp, i64, vp, i64, vp, i64, i64, vp, vp, vp, vp, vp]
+    lib.fedattn_dequantize_kv.restype = C.c_int
+    lib.fedattn_dequantize_kv.argtypes = [vp, C.POINTER(Shape), i64, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+    lib.fedattn_decode_quant.restype = C.c_int
+    lib.fedattn_decode_quant.argtypes = [vp, C.POINTER(Shape), i32, vp, vp, vp, vp, vp, i64, vp, i32, i32, i32, vp, vp, vp]
     return lib
 
 
@@ -362,3 +372,160 @@ def fedattn_decode_noalloc(shape: Shape, mode: int, q, k_cache, v_cache, cache_s
     _check(_lib.fedattn_decode_noalloc(C.byref(shape), int(mode), _ptr(q), _ptr(k_cache), _ptr(v_cache),
                                        int(cache_stride_participant), _ptr(kv_len), int(max_kv_len), _ptr(o),
                                        _ptr(lse), _stream(stream)), "fedattn_decode_noalloc")
+
+
+# ---- queries and keys before attention, and the 4-bit cache -------------------------------------------------------------
+# These calls take tensors of several kinds; what the C call cannot see (types, shapes, strides) is checked here.
+def _stream_of(ctx: Context, stream) -> int:
+    """The current stream of the context's device, which need not be the current device."""
+    if stream is None and _raw_stream is not None and torch.cuda.is_initialized():
+        return _raw_stream(ctx.device)
+    return torch.cuda.current_stream(ctx.device).cuda_stream if stream is None else _stream(stream)
+
+
+def _tensor(ctx: Context, t, dtype, shape, what: str):
+    """Pointer of a contiguous tensor of this type and shape on the context's device; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (what, dtype, tuple(shape), t.dtype, tuple(t.shape)))
+    if t.device.index != ctx.device:
+        raise ValueError("%s must be on device %d" % (what, ctx.device))
+    return _ptr(t)
+
+
+def _rows(ctx: Context, t, n_rows: int, heads: int, shape: Shape, what: str):
+    """Pointer and row stride (in elements, 0 for packed) of [n_rows, heads, head_dim] whose rows are contiguous."""
+    if t is None:
+        return None, 0
+    d = shape.head_dim
+    if t.dtype != shape.torch_dtype or tuple(t.shape) != (n_rows, heads, d):
+        raise ValueError("%s must be %s of shape %s, not %s of shape %s" % (what, shape.torch_dtype, (n_rows, heads, d), t.dtype,
+                                                                             tuple(t.shape)))
+    if t.device.index != ctx.device:
+        raise ValueError("%s must be on device %d" % (what, ctx.device))
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d) or (n_rows > 1 and t.stride(0) < heads * d):
+        raise ValueError("%s: the heads of a row must be contiguous, and rows must not overlap" % what)
+    return t.data_ptr(), t.stride(0) if n_rows > 1 else 0
+
+
+def _args_qk_norm_rope(ctx, shape, q, k, q_weight, k_weight, eps, pos, inv_freq, interleaved, q_out, k_out, stream):
+    if q is None and k is None:
+        raise ValueError("need q or k")
+    n = int((q if q is not None else k).shape[0])
+    hq, hkv, d, dt = shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.torch_dtype
+    qp, qs = _rows(ctx, q, n, hq, shape, "q")
+    kp, ks = _rows(ctx, k, n, hkv, shape, "k")
+    freq = None if inv_freq is None or len(inv_freq) == 0 else (C.c_double * len(inv_freq))(*[float(x) for x in inv_freq])
+    return (ctx.handle, C.byref(shape), n, qp, qs, kp, ks, _tensor(ctx, q_weight, dt, (d,), "q_weight"),
+            _tensor(ctx, k_weight, dt, (d,), "k_weight"), float(eps), _tensor(ctx, pos, torch.int32, (n,), "pos"), freq,
+            2 * len(freq) if freq is not None else 0, int(bool(interleaved)), _tensor(ctx, q_out, dt, (n, hq, d), "q_out"),
+            _tensor(ctx, k_out, dt, (n, hkv, d), "k_out"), _stream_of(ctx, stream))
+
+
+def fedattn_qk_norm_rope(ctx: Context, shape: Shape, q, k, q_weight, k_weight, eps: float, pos, inv_freq: Sequence[float],
+                         interleaved: bool, q_out, k_out, stream=None):
+    """RMS norm per head of queries and keys, then the rotation by position.  q [n, Hq, d] and k [n, Hkv, d] may be strided
+    over rows (slices of joint projections); inv_freq: rot_dim / 2 host numbers, radians per position."""
+    _check(_lib.fedattn_qk_norm_rope(*_args_qk_norm_rope(ctx, shape, q, k, q_weight, k_weight, eps, pos, inv_freq, interleaved,
+                                                         q_out, k_out, stream)), "fedattn_qk_norm_rope")
+
+
+def prepare_qk_norm_rope(ctx: Context, shape: Shape, q, k, q_weight, k_weight, eps: float, pos, inv_freq: Sequence[float],
+                         interleaved: bool, q_out, k_out, stream=None):
+    return PreparedCall(_lib.fedattn_qk_norm_rope,
+                        _args_qk_norm_rope(ctx, shape, q, k, q_weight, k_weight, eps, pos, inv_freq, interleaved, q_out, k_out,
+                                           stream),
+                        "fedattn_qk_norm_rope", (ctx, shape, q, k, q_weight, k_weight, pos, q_out, k_out))
+
+
+class QuantCache:
+    """The four device arrays of 4-bit caches: codes uint8 [n_caches, Hkv, cap_rows, d/2], scales uint8
+    [n_caches, Hkv, cap_rows, d/32], for keys and for values.  cap_rows: multiple of 16.  Arrays that are not given are
+    allocated, zeroed."""
+
+    def __init__(self, shape: Shape, n_caches: int, cap_rows: int, k_codes=None, k_scales=None, v_codes=None, v_scales=None,
+                 device: int = 0):
+        self.n_caches, self.cap_rows = int(n_caches), int(cap_rows)
+        if shape.head_dim % 32 or self.cap_rows % 16 or self.cap_rows < 0 or self.n_caches < 1:
+            raise ValueError("4-bit caches need head_dim a multiple of 32 and cap_rows a multiple of 16")
+        rows = (self.n_caches, shape.n_kv_heads, self.cap_rows)
+        given = {"k_codes": k_codes, "k_scales": k_scales, "v_codes": v_codes, "v_scales": v_scales}
+        for name, t in given.items():
+            want = rows + (shape.head_dim // (2 if name.endswith("codes") else 32),)
+            if t is None:
+                t = torch.zeros(want, dtype=torch.uint8, device="cuda:%d" % device)
+            if t.dtype != torch.uint8 or tuple(t.shape) != want or not t.is_contiguous() or t.device.type != "cuda":
+                raise ValueError("%s must be contiguous uint8 of shape %s on a GPU" % (name, want))
+            setattr(self, name, t)
+
+    def arrays(self):
+        return self.k_codes, self.k_scales, self.v_codes, self.v_scales
+
+
+def _cache(ctx, shape, cache: QuantCache):
+    rows = (cache.n_caches, shape.n_kv_heads, cache.cap_rows)
+    return [_tensor(ctx, t, torch.uint8, rows + (w,), "cache") for t, w in
+            zip(cache.arrays(), (shape.head_dim // 2, shape.head_dim // 32) * 2)]
+
+
+def _args_quantize_kv(ctx, shape, k, v, at, cache, stream):
+    n = int(k.shape[0])
+    kp, ks = _rows(ctx, k, n, shape.n_kv_heads, shape, "k")
+    vp, vs = _rows(ctx, v, n, shape.n_kv_heads, shape, "v")
+    return (ctx.handle, C.byref(shape), n, kp, ks, vp, vs, _tensor(ctx, at, torch.int32, (n,), "at"), cache.n_caches,
+            cache.cap_rows, *_cache(ctx, shape, cache), _stream_of(ctx, stream))
+
+
+def fedattn_quantize_kv(ctx: Context, shape: Shape, k, v, at, cache: QuantCache, stream=None):
+    """Rows of k, v [n, Hkv, d] (strided over rows or packed) into 4-bit caches: row i to flat row at[i] (int32, distinct;
+    negative: skipped; None: i)."""
+    _check(_lib.fedattn_quantize_kv(*_args_quantize_kv(ctx, shape, k, v, at, cache, stream)), "fedattn_quantize_kv")
+
+
+def prepare_quantize_kv(ctx: Context, shape: Shape, k, v, at, cache: QuantCache, stream=None):
+    return PreparedCall(_lib.fedattn_quantize_kv, _args_quantize_kv(ctx, shape, k, v, at, cache, stream), "fedattn_quantize_kv",
+                        (ctx, shape, k, v, at, cache))
+
+
+def _args_dequantize_kv(ctx, shape, cache, at, k, v, stream):
+    n, dt = int(k.shape[0]), shape.torch_dtype
+    rows = (n, shape.n_kv_heads, shape.head_dim)
+    return (ctx.handle, C.byref(shape), n, _tensor(ctx, at, torch.int32, (n,), "at"), cache.n_caches, cache.cap_rows,
+            *_cache(ctx, shape, cache), _tensor(ctx, k, dt, rows, "k"), _tensor(ctx, v, dt, rows, "v"), _stream_of(ctx, stream))
+
+
+def fedattn_dequantize_kv(ctx: Context, shape: Shape, cache: QuantCache, at, k, v, stream=None):
+    """The values of flat rows at[i] of 4-bit caches (None: rows 0, 1, ...) to rows i of k, v [n, Hkv, d]."""
+    _check(_lib.fedattn_dequantize_kv(*_args_dequantize_kv(ctx, shape, cache, at, k, v, stream)), "fedattn_dequantize_kv")
+
+
+def prepare_dequantize_kv(ctx: Context, shape: Shape, cache: QuantCache, at, k, v, stream=None):
+    return PreparedCall(_lib.fedattn_dequantize_kv, _args_dequantize_kv(ctx, shape, cache, at, k, v, stream),
+                        "fedattn_dequantize_kv", (ctx, shape, cache, at, k, v))
+
+
+def _args_decode_quant(ctx, shape, mode, q, cache, kv_len, max_kv_len, o, lse, window, n_sink, stream):
+    n = shape.n_participants
+    caches = 1 if int(mode) == DECODE_SYNC else n
+    if cache.n_caches != caches:
+        raise ValueError("need %d caches, not %d" % (caches, cache.n_caches))
+    rows = (n, shape.n_q_heads, shape.head_dim)
+    return (ctx.handle, C.byref(shape), int(mode), _tensor(ctx, q, shape.torch_dtype, rows, "q"), *_cache(ctx, shape, cache),
+            cache.cap_rows, _tensor(ctx, kv_len, torch.int32, (caches,), "kv_len"), int(max_kv_len), int(window), int(n_sink),
+            _tensor(ctx, o, shape.torch_dtype, rows, "o"), _tensor(ctx, lse, torch.float32, rows[:2], "lse"),
+            _stream_of(ctx, stream))
+
+
+def fedattn_decode_quant(ctx: Context, shape: Shape, mode: int, q, cache: QuantCache, kv_len, max_kv_len: int, o, lse=None,
+                         window: int = 0, n_sink: int = 0, stream=None):
+    """fedattn_decode over 4-bit caches; window 0: all rows, else the last `window` and the first n_sink."""
+    _check(_lib.fedattn_decode_quant(*_args_decode_quant(ctx, shape, mode, q, cache, kv_len, max_kv_len, o, lse, window, n_sink,
+                                                         stream)), "fedattn_decode_quant")
+
+
+def prepare_decode_quant(ctx: Context, shape: Shape, mode: int, q, cache: QuantCache, kv_len, max_kv_len: int, o, lse=None,
+                         window: int = 0, n_sink: int = 0, stream=None):
+    return PreparedCall(_lib.fedattn_decode_quant,
+                        _args_decode_quant(ctx, shape, mode, q, cache, kv_len, max_kv_len, o, lse, window, n_sink, stream),
+                        "fedattn_decode_quant", (ctx, shape, q, cache, kv_len, o, lse))

@@ -108,6 +108,8 @@ size_t fedattn_workspace_bytes(const fedattn_shape *shape, int64_t max_total_tok
     size_t need = decode_scratch_bytes(shape->n_participants, shape->n_q_heads, shape->head_dim, 0);
     const size_t tab = position_table_bytes(shape->n_kv_heads, max_total_tokens, max_total_kv);
     if (tab > need) need = tab;
+    const size_t quant = decode_quant_scratch_bytes(shape->n_participants, shape->n_q_heads, shape->head_dim);
+    if (quant > need) need = quant;
     return kStatusBytes + align_up(need, 256);
 }
 
@@ -384,6 +386,143 @@ fedattn_status fedattn_decode(fedattn_ctx *ctx, const fedattn_shape *shape, int3
         err = launch_attn_generic(p, shape->dtype, max_kv_len, ctx->c.sm_count, s, &ctx->c.launches);
         if (err == cudaSuccess) front_note(ctx->c.device, s, false);
     }
+    return status_of(err);
+}
+
+fedattn_status fedattn_qk_norm_rope(fedattn_ctx *ctx, const fedattn_shape *shape, int64_t n_rows, const void *q,
+                                    int64_t q_row_stride, const void *k, int64_t k_row_stride, const void *q_weight,
+                                    const void *k_weight, float eps, const int32_t *pos, const double *inv_freq_host,
+                                    int32_t rot_dim, int32_t interleaved, void *q_out, void *k_out, fedattn_stream stream)
+{
+    if (!ctx || !shape_ok(shape) || n_rows < 0 || n_rows > 0x7fffffffLL) return FEDATTN_ERR_INVALID_ARG;
+    if (!(eps >= 0.f) || isinf(eps) || (interleaved != 0 && interleaved != 1)) return FEDATTN_ERR_INVALID_ARG;
+    const int d = shape->head_dim;
+    if (rot_dim < 0 || rot_dim > d || rot_dim % 8 != 0 || (rot_dim > 0 && !inv_freq_host)) return FEDATTN_ERR_INVALID_ARG;
+    if (!q != !q_out || !k != !k_out) return FEDATTN_ERR_INVALID_ARG;
+    RopeParams p;
+    memset(&p, 0, sizeof(p));
+    p.hq = q ? shape->n_q_heads : 0; p.hkv = k ? shape->n_kv_heads : 0;
+    const int64_t q_row = (int64_t)shape->n_q_heads * d, k_row = (int64_t)shape->n_kv_heads * d;
+    p.q_stride = q_row_stride ? q_row_stride : q_row;
+    p.k_stride = k_row_stride ? k_row_stride : k_row;
+    if (p.q_stride < q_row || p.k_stride < k_row || p.q_stride % 8 != 0 || p.k_stride % 8 != 0) return FEDATTN_ERR_INVALID_ARG;
+    for (int i = 0; i < rot_dim / 2; ++i) {
+        if (!(fabs(inv_freq_host[i]) <= 1e18)) return FEDATTN_ERR_INVALID_ARG;
+        // turns per position; whole ones do not matter
+        long double turn = fmodl((long double)inv_freq_host[i] / 6.283185307179586476925286766559L, 1.0L);
+        if (turn < 0) turn += 1.0L;
+        turn *= 18446744073709551616.0L;
+        p.freq[i] = turn >= 18446744073709551615.5L ? 0 : (uint64_t)(turn + 0.5L);
+    }
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_weight) || !aligned16(k_weight) || !aligned16(q_out) || !aligned16(k_out))
+        return FEDATTN_ERR_INVALID_ARG;
+    if ((q && q == q_out && p.q_stride != q_row) || (k && k == k_out && p.k_stride != k_row)) return FEDATTN_ERR_INVALID_ARG;
+    if (n_rows == 0 || (!q && !k)) return FEDATTN_OK;
+    DeviceGuard g(ctx->c.device);
+    if (g.err != cudaSuccess) return status_of(g.err);
+    p.q = q; p.k = k; p.wq = q_weight; p.wk = k_weight; p.qo = q_out; p.ko = k_out;
+    p.n_rows = n_rows; p.d = d; p.rot = rot_dim; p.interleaved = interleaved; p.eps = eps; p.pos = pos;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t err = launch_qk_norm_rope(p, shape->dtype, ctx->c.sm_count, s, &ctx->c.launches);
+    if (err == cudaSuccess) front_note(ctx->c.device, s, false);
+    return status_of(err);
+}
+
+}  // extern "C"
+
+namespace {
+
+// What the calls on 4-bit caches have in common.
+fedattn_status quant_ok(const fedattn_ctx *ctx, const fedattn_shape *shape, int64_t n_caches, int64_t cap, const void *k_codes,
+                        const void *k_scales, const void *v_codes, const void *v_scales)
+{
+    if (!ctx || !shape_ok(shape) || n_caches < 1 || cap < 0 || cap % 16 != 0) return FEDATTN_ERR_INVALID_ARG;
+    if (cap > 0x7fffffffLL || n_caches > 0x7fffffffLL || n_caches * cap > 0x7fffffffLL) return FEDATTN_ERR_INVALID_ARG;
+    if (shape->head_dim % 32 != 0) return FEDATTN_ERR_UNSUPPORTED;
+    if (cap > 0 && (!k_codes || !k_scales || !v_codes || !v_scales)) return FEDATTN_ERR_INVALID_ARG;
+    if (!aligned16(k_codes) || !aligned16(k_scales) || !aligned16(v_codes) || !aligned16(v_scales)) return FEDATTN_ERR_INVALID_ARG;
+    return FEDATTN_OK;
+}
+
+fedattn_status quant_rows(fedattn_ctx *ctx, const fedattn_shape *shape, QuantRows &p, bool back, fedattn_stream stream)
+{
+    DeviceGuard g(ctx->c.device);
+    if (g.err != cudaSuccess) return status_of(g.err);
+    p.hkv = shape->n_kv_heads;
+    p.status = ctx->c.status;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t err = launch_quant_rows(p, back, shape->dtype, shape->head_dim, s, &ctx->c.launches);
+    if (err == cudaSuccess) front_note(ctx->c.device, s, false);
+    return status_of(err);
+}
+
+}  // namespace
+
+extern "C" {
+
+fedattn_status fedattn_quantize_kv(fedattn_ctx *ctx, const fedattn_shape *shape, int64_t n_rows, const void *k,
+                                   int64_t k_row_stride, const void *v, int64_t v_row_stride, const int32_t *at,
+                                   int64_t n_caches, int64_t cap_rows, uint8_t *k_codes, uint8_t *k_scales, uint8_t *v_codes,
+                                   uint8_t *v_scales, fedattn_stream stream)
+{
+    const fedattn_status st = quant_ok(ctx, shape, n_caches, cap_rows, k_codes, k_scales, v_codes, v_scales);
+    if (st != FEDATTN_OK) return st;
+    if (n_rows < 0 || n_rows > 0x7fffffffLL || (!at && n_rows > n_caches * cap_rows)) return FEDATTN_ERR_INVALID_ARG;
+    const int64_t row = (int64_t)shape->n_kv_heads * shape->head_dim;
+    QuantRows p;
+    memset(&p, 0, sizeof(p));
+    p.k_stride = k_row_stride ? k_row_stride : row;
+    p.v_stride = v_row_stride ? v_row_stride : row;
+    if (p.k_stride < row || p.v_stride < row || p.k_stride % 8 != 0 || p.v_stride % 8 != 0) return FEDATTN_ERR_INVALID_ARG;
+    if (n_rows == 0) return FEDATTN_OK;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return FEDATTN_ERR_INVALID_ARG;
+    p.k = k; p.v = v; p.n_rows = n_rows; p.n_caches = n_caches; p.cap = cap_rows; p.at = at;
+    p.k_codes = k_codes; p.k_scales = k_scales; p.v_codes = v_codes; p.v_scales = v_scales;
+    return quant_rows(ctx, shape, p, false, stream);
+}
+
+fedattn_status fedattn_dequantize_kv(fedattn_ctx *ctx, const fedattn_shape *shape, int64_t n_rows, const int32_t *at,
+                                     int64_t n_caches, int64_t cap_rows, const uint8_t *k_codes, const uint8_t *k_scales,
+                                     const uint8_t *v_codes, const uint8_t *v_scales, void *k, void *v, fedattn_stream stream)
+{
+    const fedattn_status st = quant_ok(ctx, shape, n_caches, cap_rows, k_codes, k_scales, v_codes, v_scales);
+    if (st != FEDATTN_OK) return st;
+    if (n_rows < 0 || n_rows > 0x7fffffffLL || (!at && n_rows > n_caches * cap_rows)) return FEDATTN_ERR_INVALID_ARG;
+    if (n_rows == 0) return FEDATTN_OK;
+    if (!k || !v || !aligned16(k) || !aligned16(v)) return FEDATTN_ERR_INVALID_ARG;
+    QuantRows p;
+    memset(&p, 0, sizeof(p));
+    p.k_out = k; p.v_out = v; p.n_rows = n_rows; p.n_caches = n_caches; p.cap = cap_rows; p.at = at;
+    p.k_codes = const_cast<uint8_t *>(k_codes); p.k_scales = const_cast<uint8_t *>(k_scales);
+    p.v_codes = const_cast<uint8_t *>(v_codes); p.v_scales = const_cast<uint8_t *>(v_scales);
+    return quant_rows(ctx, shape, p, true, stream);
+}
+
+fedattn_status fedattn_decode_quant(fedattn_ctx *ctx, const fedattn_shape *shape, int32_t mode, const void *q,
+                                    const uint8_t *k_codes, const uint8_t *k_scales, const uint8_t *v_codes,
+                                    const uint8_t *v_scales, int64_t cap_rows, const int32_t *kv_len, int32_t max_kv_len,
+                                    int32_t window, int32_t n_sink, void *o, float *lse, fedattn_stream stream)
+{
+    if (!shape_ok(shape) || (mode != FEDATTN_DECODE_LOCAL && mode != FEDATTN_DECODE_SYNC)) return FEDATTN_ERR_INVALID_ARG;
+    const int N = shape->n_participants;
+    const fedattn_status st = quant_ok(ctx, shape, mode == FEDATTN_DECODE_SYNC ? 1 : N, cap_rows, k_codes, k_scales, v_codes, v_scales);
+    if (st != FEDATTN_OK) return st;
+    if (!q || !o || !kv_len || !aligned16(q) || !aligned16(o) || max_kv_len < 0 || max_kv_len > cap_rows) return FEDATTN_ERR_INVALID_ARG;
+    if (window < 0 || n_sink < 0 || (window == 0 && n_sink > 0)) return FEDATTN_ERR_INVALID_ARG;
+    const size_t need = decode_quant_scratch_bytes(N, shape->n_q_heads, shape->head_dim);
+    if (ctx->c.scratch_bytes < need) return FEDATTN_ERR_WORKSPACE;
+    DeviceGuard g(ctx->c.device);
+    if (g.err != cudaSuccess) return status_of(g.err);
+    QuantDecodeParams p;
+    memset(&p, 0, sizeof(p));
+    p.q = q; p.k_codes = k_codes; p.k_scales = k_scales; p.v_codes = v_codes; p.v_scales = v_scales; p.o = o; p.lse = lse;
+    p.n_part = N; p.hq = shape->n_q_heads; p.hkv = shape->n_kv_heads; p.d = shape->head_dim; p.scale = eff_scale(shape);
+    p.sync = mode == FEDATTN_DECODE_SYNC; p.cap = cap_rows; p.kv_len = kv_len; p.max_kv_len = max_kv_len;
+    p.window = window; p.n_sink = n_sink;
+    p.partial = reinterpret_cast<float *>(ctx->c.scratch); p.partial_bytes = ctx->c.scratch_bytes;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t err = launch_decode_quant(p, shape->dtype, ctx->c.device, ctx->c.sm_count, s, &ctx->c.launches);
+    if (err == cudaSuccess) front_note(ctx->c.device, s, false);
     return status_of(err);
 }
 

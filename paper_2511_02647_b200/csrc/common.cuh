@@ -239,4 +239,46 @@ struct DecodeParams {
 size_t decode_scratch_bytes(int n_part, int hq, int d, int sm_count);
 cudaError_t launch_decode_bf16(const Context *ctx, const DecodeParams &p, cudaStream_t s, int64_t *launches);
 
+// ---- norm of queries and keys with their rotation ----------------------------------------------------
+struct RopeParams {
+    const void *q, *k, *wq, *wk;  // weights: nullable
+    void *qo, *ko;
+    int64_t n_rows, q_stride, k_stride;          // elements between rows
+    int32_t hq, hkv, d, rot, interleaved;
+    float eps;
+    const int32_t *pos;           // nullable (= row index)
+    uint64_t freq[FEDATTN_MAX_HEAD_DIM / 2];     // turns per position, in units of 2^-64, modulo a turn
+};
+cudaError_t launch_qk_norm_rope(const RopeParams &p, int dtype, int sm_count, cudaStream_t s, int64_t *launches);
+
+// ---- the 4-bit cache ------------------------------------------------------------------------------------
+struct QuantRows {
+    const void *k, *v;            // rows to write
+    void *k_out, *v_out;          // rows to read back
+    int64_t k_stride, v_stride;   // elements between the rows of k, v
+    int64_t n_rows, n_caches, cap;
+    int32_t hkv;
+    const int32_t *at;            // nullable (= row index): cache * cap + row; negative: none
+    uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    int32_t *status;
+};
+cudaError_t launch_quant_rows(const QuantRows &p, bool back, int dtype, int d, cudaStream_t s, int64_t *launches);
+
+struct QuantDecodeParams {
+    const void *q;
+    const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+    void *o;
+    float *lse;
+    int32_t n_part, hq, hkv, d;
+    float scale;
+    int32_t sync;
+    int64_t cap;
+    const int32_t *kv_len;
+    int32_t max_kv_len, window, n_sink;          // window 0: every key
+    float *partial;               // scratch
+    size_t partial_bytes;
+};
+size_t decode_quant_scratch_bytes(int n_part, int hq, int d);
+cudaError_t launch_decode_quant(const QuantDecodeParams &p, int dtype, int device, int sm_count, cudaStream_t s, int64_t *launches);
+
 }  // namespace fedattn

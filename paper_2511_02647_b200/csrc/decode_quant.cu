@@ -1,0 +1,622 @@
+// Decode over a cache held in 4 bits (quant_cache.cuh): one new query token per participant, local or shared caches, all
+// keys or the first n_sink and the last `window`.  A key and value of 128 channels is 136 bytes.
+//
+// Bound by issue slots rather than by memory alone: at the copy rate an SM gets 46 elements per clock, and every eight of them take 11
+// instructions to become bf16 (three shifts, four bit selections, four fma: quant_cache.cuh; nothing is rounded).  So everything else
+// is kept off that path:
+//   * Both products stand on their side, S^T = K Q^T and O^T = V^T P^T.  Keys and channels are the 16 rows of an mma.sync.m16n8k16, the
+//     query rows that share a KV head its 8 columns: a group of 4 heads wastes half a tile, not three quarters, and takes half the
+//     products and accumulators.
+//   * The nibbles come out of a word in pairs (i, i + 4); which channel, or key, stands at which place of a sum is free, so Q and the keys
+//     are placed to fit.  K: a lane's quarter of the row is one vector load, its nibbles are operand A as they come.  V: the halves of two keys'
+//     words side by side (one byte permutation for eight elements) make the pairs that run along the keys.
+//   * A warp has tiles of 32 keys of its own and its own ring of asynchronous copies: no barrier between warps during the walk.  Head-major
+//     rows make every copy a run of consecutive bytes.
+// The exponent reference follows every new maximum, so the heaviest key weighs 1, which bf16 holds.  fp32 queries go in as three bf16
+// parts, and so do their weights (24 bits): six products for two.
+//
+// Up to 8 splits of a (cache, KV head) are one cluster and one launch; more are merged by a second kernel out of the workspace.
+#include <cooperative_groups.h>
+#include <string.h>
+
+#include "quant_cache.cuh"
+
+namespace fedattn {
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kTileKeys = 32;
+constexpr int kMaxSlots = 64;                                   // partials per output row in the workspace
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// transposes an 8 x 8 matrix of 16-bit values that the warp holds, a pair per lane
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// the leading 8 bits of two values as a bf16 pair; what is left stays in them
+__device__ __forceinline__ uint32_t take_part(float &lo, float &hi)
+{
+    const uint32_t a = __float_as_uint(lo), b = __float_as_uint(hi);
+    lo -= __uint_as_float(a & 0xffff0000u);
+    hi -= __uint_as_float(b & 0xffff0000u);
+    return __byte_perm(a, b, 0x7632);
+}
+// partials, past L1 (volatile: behind the wait for the kernel that wrote them)
+__device__ __forceinline__ float2 ld_partial2(const float *p)
+{
+    float2 v;
+    asm volatile("ld.global.cg.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float4 ld_partial4(const float *p)
+{
+    float4 v;
+    asm volatile("ld.global.cg.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ void store4(float *p, float4 v) { *reinterpret_cast<float4 *>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v)
+{
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+__device__ __forceinline__ float load1(const float *p) { return *p; }
+__device__ __forceinline__ float load1(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+
+// Which keys a cache of `len` rows shows: [0, a) and [b, len).  The walk goes over tiles of kTileKeys keys: 0 .. n_a - 1, then t_b ...
+struct Walk {
+    int a, b, len, n_a, t_b, n_tiles;
+    __device__ Walk(const QuantDecodeParams &p, int cache)
+    {
+        len = max(0, min(ld_int(p.kv_len + (p.sync ? 0 : cache)), p.max_kv_len));
+        a = len; b = len;
+        if (p.window > 0 && p.window < len) { b = len - p.window; a = min(p.n_sink, b); }
+        const int n_t = (len + kTileKeys - 1) / kTileKeys;
+        n_a = (a + kTileKeys - 1) / kTileKeys;
+        t_b = max(b / kTileKeys, n_a);
+        n_tiles = n_a + (b < len ? n_t - t_b : 0);
+    }
+    __device__ int key0(int tile) const { return (tile < n_a ? tile : t_b + (tile - n_a)) * kTileKeys; }
+    __device__ bool sees(int key) const { return key < a || (key >= b && key < len); }
+};
+
+// T: type of q and o; kD: channels; kNT: column tiles of 8 query rows; kOneLaunch: the splits are a cluster.
+template <typename T, int kD, int kNT> struct Layout {
+    static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;       // bf16 parts of queries and weights
+    static constexpr int kW = kD / 32;                          // words of a lane's quarter of a key: 8 channels each
+    static constexpr int kCodeRow = kD / 2, kScaleRow = kD / kQuantGroup;                 // bytes
+    static constexpr int kCodeBytes = kTileKeys * kCodeRow, kScaleBytes = kTileKeys * kScaleRow;
+    static constexpr int kStageBytes = 2 * (kCodeBytes + kScaleBytes);
+    static constexpr int kStages = 4;
+    static constexpr int kRing = kStages * kStageBytes;         // of a warp
+    static constexpr int kQBytes = kParts * kNT * 8 * kD * 2;
+    static constexpr int kPartialRow = kD + 4;                  // m, l, 2 pad, o
+    static constexpr int kPartialBytes = kWarps * kNT * 8 * kPartialRow * 4;
+    static constexpr int kRingBytes = kWarps * kRing > kPartialBytes ? kWarps * kRing : kPartialBytes;
+    static constexpr int kBytes = kQBytes + kRingBytes;
+    static constexpr bool kQInRegs = kNT * kParts <= 2;
+};
+
+template <typename T, int kD, int kNT, bool kOneLaunch>
+__global__ void __launch_bounds__(kThreads, kNT == 4 || sizeof(T) == 4 ? 2 : 3)
+decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, int n_chunks)
+{
+    using L = Layout<T, kD, kNT>;
+    constexpr int kW = L::kW, kKs = 2 * kW, kParts = L::kParts, kRows = 8 * kNT, kMt = kD / 16, kStages = L::kStages;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, t = lane & 3;
+    grid_wait();                                                // nothing is read or written before
+    // (the merge kernel of this call, the only grid that can follow, waits for this one's end before it reads)
+    if (!kOneLaunch) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int split = blockIdx.x, kvh = blockIdx.y;
+    const int cache = blockIdx.z / n_chunks, chunk = blockIdx.z - cache * n_chunks;
+    const int g = p.hq / p.hkv;
+    const int rows_total = p.sync ? p.n_part * g : g;           // query rows that share this cache and KV head
+    const int rows_here = min(kRows, rows_total - chunk * kRows);
+    auto out_row = [&](int srow) -> int64_t {                   // stacked row -> row of q and o
+        const int part = p.sync ? srow / g : cache, sub = p.sync ? srow - part * g : srow;
+        return (int64_t)part * p.hq + kvh * g + sub;
+    };
+
+    const Walk walk(p, cache);
+    const int per = (walk.n_tiles + n_splits - 1) / n_splits;
+    const int tile_lo = min(split * per, walk.n_tiles), tile_hi = min(tile_lo + per, walk.n_tiles);
+    const int64_t row0 = ((int64_t)cache * p.hkv + kvh) * p.cap;
+    const uint8_t *kc = p.k_codes + row0 * L::kCodeRow, *ks = p.k_scales + row0 * L::kScaleRow;
+    const uint8_t *vc = p.v_codes + row0 * L::kCodeRow, *vs = p.v_scales + row0 * L::kScaleRow;
+
+    uint8_t *ring = smem + L::kQBytes + warp * L::kRing;
+    // Pieces of 16 bytes.  Rows are copied up to the length, rounded up to 16 rows (the cache has them); what lies behind that in a tile is
+    // whatever was there: finite, and masked.  128 channels: the pieces of rows 2, 3, 6, 7, .. of V change places in pairs, which
+    // spreads the reads of rows t over the banks.
+    auto load_tile = [&](int tile, int stage) {
+        const int key0 = walk.key0(tile), rows = min(kTileKeys, (walk.len - key0 + 15) & ~15);
+        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring + stage * L::kStageBytes);
+        const uint8_t *k_src = kc + (int64_t)key0 * L::kCodeRow, *v_src = vc + (int64_t)key0 * L::kCodeRow;
+        constexpr int kPieces = L::kCodeBytes / 16, kRowPieces = L::kCodeRow / 16;
+#pragma unroll
+        for (int i0 = 0; i0 < kPieces; i0 += 32) {
+            const int i = i0 + lane;
+            const int j = kD == 128 ? i ^ ((i >> 2) & 2) : i;   // (row i / 4: bit 1 of it flips bit 1 of the piece)
+            if (i < rows * kRowPieces) {
+                cp_async16(dst + i * 16, k_src + i * 16);
+                cp_async16(dst + L::kCodeBytes + j * 16, v_src + i * 16);
+            }
+        }
+        const uint8_t *s_src = lane < 16 ? ks : vs;
+        const int i = lane & 15;
+        if (i < rows * L::kScaleRow / 16)
+            cp_async16(dst + 2 * L::kCodeBytes + (lane >> 4) * L::kScaleBytes + i * 16, s_src + (int64_t)key0 * L::kScaleRow + i * 16);
+    };
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) {
+        if (tile_lo + warp + s * kWarps < tile_hi) load_tile(tile_lo + warp + s * kWarps, s);
+        cp_async_commit();
+    }
+
+    // ---- Q as operand B: [part][column tile][step][lane] pairs of pairs ----
+    // Step 2 w + h of a lane: word w of its quarter of the channels, nibble pairs 2 h and 2 h + 1 (nibbles i and i + 4).
+    uint2 *sq = reinterpret_cast<uint2 *>(smem);
+    for (int i = tid; i < kRows * (kD / 8); i += kThreads) {
+        const int row = i / (kD / 8), x = i - row * (kD / 8);   // word x of the row's channels
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        if (row < rows_here) {
+            const T *src = static_cast<const T *>(p.q) + out_row(chunk * kRows + row) * kD + 8 * x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = load1(src + e);
+        }
+        const int qt = x / kW, w = x - qt * kW;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            uint32_t pr[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) pr[e] = take_part(v[e], v[e + 4]);
+            uint2 *dst = sq + ((part * kNT + (row >> 3)) * kKs + 2 * w) * 32 + (row & 7) * 4 + qt;
+            dst[0] = make_uint2(pr[0], pr[1]);
+            dst[32] = make_uint2(pr[2], pr[3]);
+        }
+    }
+    __syncthreads();
+    uint2 qf[L::kQInRegs ? kNT * kParts : 1][kKs];
+    if (L::kQInRegs) {
+#pragma unroll
+        for (int n = 0; n < kNT * kParts; ++n)
+#pragma unroll
+            for (int s = 0; s < kKs; ++s) qf[n][s] = sq[(n * kKs + s) * 32 + lane];
+    }
+
+    const float sl2 = p.scale * 1.4426950408889634f;
+    float m[kNT][2], l[kNT][2];                                 // query rows 2 t, 2 t + 1 of a column tile
+    float acc[kNT][kMt][4];                                     // O^T: channels (kD / 8) r + 2 i, + 1 by rows 2 t, 2 t + 1
+#pragma unroll
+    for (int n = 0; n < kNT; ++n) {
+        m[n][0] = m[n][1] = -INFINITY;
+        l[n][0] = l[n][1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < kMt; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
+    }
+    // Key of row i of a 16-row operand: i = 2 t + e (+ 8) stands for key t + 4 e (+ 8).
+    const int my_key = (r >> 1) + 4 * (r & 1);
+    int stage = 0;
+#pragma unroll 1
+    for (int tile = tile_lo + warp; tile < tile_hi; tile += kWarps) {
+        cp_async_wait<kStages - 2>();
+        __syncwarp();
+        {
+            const int next = tile + (kStages - 1) * kWarps, st = stage == 0 ? kStages - 1 : stage - 1;
+            if (next < tile_hi) load_tile(next, st);
+            cp_async_commit();
+        }
+        const uint8_t *sK = ring + stage * L::kStageBytes, *sV = sK + L::kCodeBytes;
+        const uint8_t *sKs = sV + L::kCodeBytes, *sVs = sKs + L::kScaleBytes;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+
+        // ---- S^T = K Q^T: two row tiles of 16 keys ----
+        float s[2][kNT][4];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int n = 0; n < kNT; ++n) s[mt][n][0] = s[mt][n][1] = s[mt][n][2] = s[mt][n][3] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            uint32_t code[2][kW];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint8_t *src = sK + (16 * mt + 8 * e + my_key) * L::kCodeRow + t * (kD / 8);
+                if (kW == 4) {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(src);
+                    code[e][0] = x.x; code[e][1] = x.y; code[e][2 % kW] = x.z; code[e][3 % kW] = x.w;
+                } else if (kW == 2) {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(src);
+                    code[e][0] = x.x; code[e][1 % kW] = x.y;
+                } else {
+#pragma unroll
+                    for (int w = 0; w < kW; ++w) code[e][w] = reinterpret_cast<const uint32_t *>(src)[w];
+                }
+            }
+            uint32_t sc[2], of[2];
+#pragma unroll
+            for (int w = 0; w < kW; ++w) {
+                if (w == 0 || kW == 3) {                        // the group of this word; 96 channels: a quarter may touch two
+                    const int grp = (t * kW + w) >> 2;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        sc[e] = scale_pair(sKs[(16 * mt + 8 * e + my_key) * L::kScaleRow + grp] * 0x10001u);
+                        of[e] = offset_pair(sc[e]);
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t a[4];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        a[e] = h ? nibble_pair<2>(code[e][w], sc[e], of[e]) : nibble_pair<0>(code[e][w], sc[e], of[e]);
+                        a[2 + e] = h ? nibble_pair<3>(code[e][w], sc[e], of[e]) : nibble_pair<1>(code[e][w], sc[e], of[e]);
+                    }
+#pragma unroll
+                    for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                        for (int n = 0; n < kNT; ++n) {
+                            const uint2 b = L::kQInRegs ? qf[part * kNT + n][2 * w + h] : sq[((part * kNT + n) * kKs + 2 * w + h) * 32 + lane];
+                            mma_bf16(s[mt][n], a, b.x, b.y);
+                        }
+                }
+            }
+        }
+        // ---- mask, online softmax: a row's 32 keys are 4 values in each of the 8 lanes with the same t ----
+        const int key0 = walk.key0(tile);
+        const bool full = key0 + kTileKeys <= walk.a || (key0 >= walk.b && key0 + kTileKeys <= walk.len);
+        uint32_t pf[kParts][kNT][2][2];                         // P^T as operand B: [row tile of keys][half]
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) {
+            float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const bool see = full || walk.sees(key0 + 16 * mt + 8 * (c >> 1) + my_key);
+                    s[mt][n][c] = see ? s[mt][n][c] * sl2 : -INFINITY;
+                    mx[c & 1] = fmaxf(mx[c & 1], s[mt][n][c]);
+                }
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) {
+                mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
+                mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
+            }
+            if (__any_sync(0xffffffffu, mx[0] > m[n][0] || mx[1] > m[n][1])) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float mn = fmaxf(m[n][e], mx[e]), al = mn == -INFINITY ? 1.f : ex2(m[n][e] - mn);
+                    m[n][e] = mn;
+                    l[n][e] *= al;
+#pragma unroll
+                    for (int i = 0; i < kMt; ++i) { acc[n][i][e] *= al; acc[n][i][2 + e] *= al; }
+                }
+            }
+            const float ref[2] = {m[n][0] == -INFINITY ? 0.f : m[n][0], m[n][1] == -INFINITY ? 0.f : m[n][1]};
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    s[mt][n][c] = ex2(s[mt][n][c] - ref[c & 1]);
+                    l[n][c & 1] += s[mt][n][c];
+                }
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        pf[part][n][mt][e] = transpose8(kParts > 1 ? take_part(s[mt][n][2 * e], s[mt][n][2 * e + 1])
+                                                                   : pack_bf16(s[mt][n][2 * e], s[mt][n][2 * e + 1]));
+        }
+        // ---- O^T += V^T P^T ----
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+            // keys 16 mt + 8 e + t + 4 f: half e of the step, member f of the pair
+            uint32_t code[2][2][kW > 1 ? (kW + 1) / 2 : 1];     // this lane's kD / 8 channels: kW half-words
+            uint32_t sc[2], of[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int f = 0; f < 2; ++f) {
+                    const int key = 16 * mt + 8 * e + 4 * f + t;
+                    const uint8_t *src = sV + key * L::kCodeRow;
+                    if (kW == 4) {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(src + (((r >> 1) ^ (t & 2)) << 4) + 8 * (r & 1));
+                        code[e][f][0] = x.x; code[e][f][kW > 2 ? 1 : 0] = x.y;
+                    } else if (kW == 2) {
+                        code[e][f][0] = *reinterpret_cast<const uint32_t *>(src + 4 * r);
+                    } else {
+                        const uint16_t *h = reinterpret_cast<const uint16_t *>(src + 2 * kW * r);
+                        code[e][f][0] = h[0];
+                        if (kW == 3) { code[e][f][0] |= (uint32_t)h[1 % kW] << 16; code[e][f][kW > 2 ? 1 : 0] = h[2 % kW]; }
+                    }
+                }
+#pragma unroll
+            for (int u = 0; u < kW; ++u) {                      // half-words: channels (kD / 8) r + 4 u .. + 3
+                if (u == 0 || kW == 3) {
+                    const int grp = ((kD / 8) * r + 4 * u) / kQuantGroup;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const uint8_t *src = sVs + (16 * mt + 8 * e + t) * L::kScaleRow + grp;
+                        sc[e] = scale_pair(src[0] | (uint32_t)src[4 * L::kScaleRow] << 16);
+                        of[e] = offset_pair(sc[e]);
+                    }
+                }
+                uint32_t v[2][4];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t x = __byte_perm(code[e][0][u >> 1], code[e][1][u >> 1], u & 1 ? 0x7632 : 0x5410);
+                    v[e][0] = nibble_pair<0>(x, sc[e], of[e]);
+                    v[e][1] = nibble_pair<1>(x, sc[e], of[e]);
+                    v[e][2] = nibble_pair<2>(x, sc[e], of[e]);
+                    v[e][3] = nibble_pair<3>(x, sc[e], of[e]);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t a[4] = {v[0][2 * i], v[0][2 * i + 1], v[1][2 * i], v[1][2 * i + 1]};
+#pragma unroll
+                    for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                        for (int n = 0; n < kNT; ++n) mma_bf16(acc[n][2 * u + i], a, pf[part][n][mt][0], pf[part][n][mt][1]);
+                }
+            }
+        }
+        __syncwarp();                                           // every lane is done with the stage that the next copies overwrite
+    }
+    cp_async_wait<0>();
+
+    // ---- partials of the warps, where the rings were ----
+    __syncthreads();
+    float *part = reinterpret_cast<float *>(smem + L::kQBytes); // [warp][row][kPartialRow]
+#pragma unroll
+    for (int n = 0; n < kNT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            float z = l[n][e];
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+            float *dst = part + (warp * kRows + 8 * n + 2 * t + e) * L::kPartialRow;
+            if (r == 0) *reinterpret_cast<float2 *>(dst) = make_float2(m[n][e], z);
+            dst += 4 + (kD / 8) * r;
+#pragma unroll
+            for (int i = 0; i < kMt; i += 2)
+                *reinterpret_cast<float4 *>(dst + 2 * i) = make_float4(acc[n][i][e], acc[n][i][2 + e], acc[n][i + 1][e], acc[n][i + 1][2 + e]);
+        }
+    __syncthreads();
+    // ---- fold the warps: a warp per row, four channels per lane; into the first warp's row, or the workspace ----
+    for (int row = warp; row < rows_here; row += kWarps) {
+        float *src = part + row * L::kPartialRow;
+        float2 ml[kWarps];
+        float mx = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kWarps; ++q) {
+            ml[q] = *reinterpret_cast<const float2 *>(src + q * kRows * L::kPartialRow);
+            mx = fmaxf(mx, ml[q].x);
+        }
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        float z = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int q = 0; q < kWarps; ++q) {
+            const float f = ex2(ml[q].x - ref);
+            z += ml[q].y * f;
+            if (4 * lane < kD) {
+                const float4 v = *reinterpret_cast<const float4 *>(src + q * kRows * L::kPartialRow + 4 + 4 * lane);
+                o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+            }
+        }
+        __syncwarp();                                           // every lane has read the maxima and sums
+        float *dst = kOneLaunch ? src : p.partial + (out_row(chunk * kRows + row) * n_splits + split) * L::kPartialRow;
+        if (lane == 0) *reinterpret_cast<float2 *>(dst) = make_float2(mx, z);
+        if (4 * lane < kD) *reinterpret_cast<float4 *>(dst + 4 + 4 * lane) = o;
+    }
+    if (!kOneLaunch) return;
+    // ---- fold the CTAs of the cluster: rank q finishes rows q, q + n_splits, ... ----
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    if (n_splits > 1) cluster.sync(); else __syncthreads();
+    for (int row = split + n_splits * warp; row < rows_here; row += n_splits * kWarps) {
+        float2 ml[kMaxCluster];
+        float4 v[kMaxCluster];
+        float mx = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) {
+            ml[q] = make_float2(-INFINITY, 0.f);
+            v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (q < n_splits) {
+                const float *src = (n_splits > 1 ? cluster.map_shared_rank(part, q) : part) + row * L::kPartialRow;
+                ml[q] = *reinterpret_cast<const float2 *>(src);
+                if (4 * lane < kD) v[q] = *reinterpret_cast<const float4 *>(src + 4 + 4 * lane);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) mx = fmaxf(mx, ml[q].x);
+        const float ref = mx == -INFINITY ? 0.f : mx;
+        float z = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int q = 0; q < kMaxCluster; ++q) {
+            const float f = ex2(ml[q].x - ref);
+            z += ml[q].y * f;
+            o.x += v[q].x * f; o.y += v[q].y * f; o.z += v[q].z * f; o.w += v[q].w * f;
+        }
+        const float inv = z > 0.f ? 1.f / z : 0.f;
+        const int64_t orow = out_row(chunk * kRows + row);
+        if (4 * lane < kD) store4(static_cast<T *>(p.o) + orow * kD + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+        if (lane == 0 && p.lse) p.lse[orow] = z > 0.f ? lse_exact(mx, z) : -INFINITY;
+    }
+    if (n_splits > 1) cluster.sync();                           // peers may still be reading this CTA's partials
+}
+
+// A CTA per output row: four groups of slots by 32 lanes of four channels.
+constexpr int kMergeGroups = 4;
+template <typename T>
+__global__ void __launch_bounds__(32 * kMergeGroups)
+decode_quant_merge_kernel(const float *partial, T *out, float *lse, int d, int n_slots)
+{
+    __shared__ float4 s_o[kMergeGroups][32];
+    __shared__ float2 s_ml[kMergeGroups];
+    grid_wait();                                                // the partials of this call
+    const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
+    const int64_t orow = blockIdx.x;
+    const float *src = partial + orow * n_slots * (d + 4);
+    const bool mine = 4 * lane < d;
+    float mm = -INFINITY, ll = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k0 = grp; k0 < n_slots; k0 += 4 * kMergeGroups) {
+        float2 ml[4];
+        float4 v[4];
+        float mn = mm;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int slot = k0 + k * kMergeGroups;
+            ml[k] = make_float2(-INFINITY, 0.f);
+            v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (slot < n_slots) {
+                ml[k] = ld_partial2(src + slot * (d + 4));
+                if (mine) v[k] = ld_partial4(src + slot * (d + 4) + 4 + 4 * lane);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mn = fmaxf(mn, ml[k].x);
+        const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(mm - ref);
+        ll *= f0; a.x *= f0; a.y *= f0; a.z *= f0; a.w *= f0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float f = ex2(ml[k].x - ref);                 // 0 for an empty partial
+            ll += ml[k].y * f;
+            a.x += v[k].x * f; a.y += v[k].y * f; a.z += v[k].z * f; a.w += v[k].w * f;
+        }
+        mm = mn;
+    }
+    s_o[grp][lane] = a;
+    if (lane == 0) s_ml[grp] = make_float2(mm, ll);
+    __syncthreads();
+    if (grp != 0) return;
+    float mx = -INFINITY, z = 0.f;
+#pragma unroll
+    for (int q = 0; q < kMergeGroups; ++q) mx = fmaxf(mx, s_ml[q].x);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int q = 0; q < kMergeGroups; ++q) {
+        const float f = ex2(s_ml[q].x - ref);
+        const float4 v = s_o[q][lane];
+        z += s_ml[q].y * f;
+        o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+    }
+    const float inv = z > 0.f ? 1.f / z : 0.f;
+    if (mine) store4(out + orow * d + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (lane == 0 && lse) lse[orow] = z > 0.f ? lse_exact(mx, z) : -INFINITY;
+}
+
+typedef void (*Kernel)(const QuantDecodeParams, int, int);
+struct Variant {
+    Kernel kernel;
+    int smem;
+};
+template <typename T, int kD, bool kOneLaunch> Variant variant_of(int nt)
+{
+    if (nt == 1) return {decode_quant_kernel<T, kD, 1, kOneLaunch>, Layout<T, kD, 1>::kBytes};
+    if (nt == 2 || sizeof(T) == 4) return {decode_quant_kernel<T, kD, 2, kOneLaunch>, Layout<T, kD, 2>::kBytes};
+    return {decode_quant_kernel<T, kD, sizeof(T) == 4 ? 2 : 4, kOneLaunch>, Layout<T, kD, sizeof(T) == 4 ? 2 : 4>::kBytes};
+}
+template <typename T, bool kOneLaunch> Variant variant_of(int d, int nt)
+{
+    switch (d) {
+    case 32: return variant_of<T, 32, kOneLaunch>(nt);
+    case 64: return variant_of<T, 64, kOneLaunch>(nt);
+    case 96: return variant_of<T, 96, kOneLaunch>(nt);
+    default: return variant_of<T, 128, kOneLaunch>(nt);
+    }
+}
+
+}  // namespace
+
+size_t decode_quant_scratch_bytes(int n_part, int hq, int d)
+{
+    return d % kQuantGroup == 0 ? (size_t)n_part * hq * kMaxSlots * (d + 4) * sizeof(float) : 0;
+}
+
+cudaError_t launch_decode_quant(const QuantDecodeParams &p, int dtype, int device, int sm_count, cudaStream_t s, int64_t *launches)
+{
+    const int g = p.hq / p.hkv, rows_total = p.sync ? p.n_part * g : g, caches = p.sync ? 1 : p.n_part;
+    const bool f32 = dtype == FEDATTN_F32;
+    const int nt = rows_total <= 8 ? 1 : (rows_total <= 16 || f32 ? 2 : 4);
+    const int n_chunks = (rows_total + 8 * nt - 1) / (8 * nt);
+    const int64_t sources = (int64_t)caches * p.hkv * n_chunks;
+    if ((int64_t)caches * n_chunks > 65535 || p.hkv > 65535) return cudaErrorInvalidValue;        // grid
+    // keys that a walk goes over, at most
+    int64_t keys = p.max_kv_len;
+    if (p.window > 0 && (int64_t)p.window + p.n_sink + 2 * kTileKeys < keys) keys = (int64_t)p.window + p.n_sink + 2 * kTileKeys;
+    const int tiles = (int)((keys + kTileKeys - 1) / kTileKeys);
+    const int per_sm = nt == 4 || f32 ? 2 : 3;                  // CTAs of an SM: one wave
+    int64_t n_splits = (int64_t)per_sm * sm_count / sources;
+    if (n_splits > tiles / kWarps) n_splits = tiles / kWarps;   // a tile per warp at the least
+    if (n_splits > kMaxSlots) n_splits = kMaxSlots;
+    if (n_splits < 1) n_splits = 1;
+    bool one_launch = n_splits <= kMaxCluster;
+    if (one_launch)
+        while (n_splits & (n_splits - 1)) n_splits &= n_splits - 1;
+    if (!one_launch && (size_t)p.n_part * p.hq * n_splits * (p.d + 4) * sizeof(float) > p.partial_bytes) return cudaErrorInvalidValue;
+    typedef __nv_bfloat16 bf;
+    const Variant v = one_launch ? (f32 ? variant_of<float, true>(p.d, nt) : variant_of<bf, true>(p.d, nt))
+                                 : (f32 ? variant_of<float, false>(p.d, nt) : variant_of<bf, false>(p.d, nt));
+    static bool attr_set[64][2][2][4][3] = {};                  // the attribute is per device
+    bool &set = attr_set[device & 63][f32][one_launch][p.d / 32 - 1][nt >> 1];
+    if (!set) {
+        const cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, v.smem);
+        if (e != cudaSuccess) return e;
+        set = true;
+    }
+    WaitFirstLaunch l(dim3((unsigned)n_splits, (unsigned)p.hkv, (unsigned)(caches * n_chunks)), dim3(kThreads), v.smem, s);
+    if (one_launch) {
+        l.attr[1].id = cudaLaunchAttributeClusterDimension;
+        l.attr[1].val.clusterDim.x = (unsigned)n_splits; l.attr[1].val.clusterDim.y = 1; l.attr[1].val.clusterDim.z = 1;
+        l.cfg.numAttrs = 2;
+    }
+    cudaError_t e = cudaLaunchKernelEx(&l.cfg, v.kernel, p, (int)n_splits, n_chunks);
+    ++*launches;
+    if (e != cudaSuccess || one_launch) return e != cudaSuccess ? e : cudaGetLastError();
+    WaitFirstLaunch ml(dim3((unsigned)(p.n_part * p.hq)), dim3(32 * kMergeGroups), 0, s);
+    const float *partial = p.partial;
+    e = f32 ? cudaLaunchKernelEx(&ml.cfg, decode_quant_merge_kernel<float>, partial, static_cast<float *>(p.o), p.lse, (int)p.d, (int)n_splits)
+            : cudaLaunchKernelEx(&ml.cfg, decode_quant_merge_kernel<bf>, partial, static_cast<bf *>(p.o), p.lse, (int)p.d, (int)n_splits);
+    ++*launches;
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace fedattn
