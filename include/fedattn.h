@@ -35,8 +35,8 @@
  *     the GPU race on its workspace.
  *   - Results are those of stream order: every call behaves as if it ran after all earlier work
  *     of its stream and before all later work.  Kernels are launched with programmatic stream
- *     serialization, in two ways.  fedattn_decode (bf16, head_dim 128), fedattn_decode_noalloc and
- *     the sparse modes of fedattn_aggregate_kv may touch their buffers before the preceding kernel
+ *     serialization, in two ways.  fedattn_decode and fedattn_decode_window (bf16, head_dim 128),
+ *     fedattn_decode_noalloc and the sparse modes of fedattn_aggregate_kv may touch their buffers before the preceding kernel
  *     of the stream has ended, and let the next one start before they end; the library tracks the
  *     buffers of such calls and holds a call back whenever that could be observed.  All others
  *     wait for everything before them before they touch anything, and let nothing start early.
@@ -334,6 +334,26 @@ fedattn_status fedattn_decode_quant(fedattn_ctx *ctx, const fedattn_shape *shape
                                     const uint8_t *v_codes, const uint8_t *v_scales, int64_t cap_rows,
                                     const int32_t *kv_len, int32_t max_kv_len, int32_t window, int32_t n_sink,
                                     void *o, float *lse, fedattn_stream stream);
+
+/* ---- attention through a sliding window with sinks -----------------------------------------------------
+ * fedattn_local_window   as fedattn_local, but row i of a segment sees row j of it only when |i - j| < window
+ *                        or j < n_sink (and j <= i when causal): a window of `window` rows that ends with, or
+ *                        without the causal mask is centred on, the row itself, and the segment's first n_sink
+ *                        rows.  Tiles in between are not read.  A windowed block over the whole sequence (a
+ *                        sync block of a windowed model) is this call with one participant.
+ * fedattn_decode_window  as fedattn_decode, but only the last `window` of the kv_len cached rows and the first
+ *                        n_sink.  With the new token's own row cached before the call it sees what the same
+ *                        row of fedattn_local_window sees.
+ * window >= 1, n_sink >= 0; either may exceed the lengths. */
+fedattn_status fedattn_local_window(fedattn_ctx *ctx, const fedattn_shape *shape,
+                                    const void *q, const void *k, const void *v,
+                                    const int32_t *cu_seqlens_host, int32_t window, int32_t n_sink,
+                                    void *o, float *lse, fedattn_stream stream);
+fedattn_status fedattn_decode_window(fedattn_ctx *ctx, const fedattn_shape *shape, int32_t mode,
+                                     const void *q, const void *k_cache, const void *v_cache,
+                                     int64_t cache_stride_participant, const int32_t *kv_len,
+                                     int32_t max_kv_len, int32_t window, int32_t n_sink,
+                                     void *o, float *lse, fedattn_stream stream);
 
 #ifdef __cplusplus
 }

@@ -25,7 +25,8 @@ _SYMBOLS = ["fedattn_workspace_bytes", "fedattn_create", "fedattn_destroy", "fed
             "fedattn_poll", "fedattn_launch_count", "fedattn_tensor_core_launch_count",
             "fedattn_selftest_wait_timeout", "fedattn_local", "fedattn_aggregate_kv",
             "fedattn_sync", "fedattn_sync_remote", "fedattn_merge", "fedattn_decode", "fedattn_decode_noalloc",
-            "fedattn_qk_norm_rope", "fedattn_quantize_kv", "fedattn_dequantize_kv", "fedattn_decode_quant"]
+            "fedattn_qk_norm_rope", "fedattn_quantize_kv", "fedattn_dequantize_kv", "fedattn_decode_quant",
+            "fedattn_local_window", "fedattn_decode_window"]
 
 
 class FedAttnError(RuntimeError):
@@ -113,6 +114,10 @@ def _load():
     lib.fedattn_decode.argtypes = [vp, C.POINTER(Shape), i32, vp, vp, vp, i64, vp, i32, vp, vp, vp]
     lib.fedattn_decode_noalloc.restype = C.c_int
     lib.fedattn_decode_noalloc.argtypes = [C.POINTER(Shape), i32, vp, vp, vp, i64, vp, i32, vp, vp, vp]
+    lib.fedattn_local_window.restype = C.c_int
+    lib.fedattn_local_window.argtypes = [vp, C.POINTER(Shape), vp, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.fedattn_decode_window.restype = C.c_int
+    lib.fedattn_decode_window.argtypes = [vp, C.POINTER(Shape), i32, vp, vp, vp, i64, vp, i32, i32, i32, vp, vp, vp]
     lib.fedattn_qk_norm_rope.restype = C.c_int
     lib.fedattn_qk_norm_rope.argtypes = [vp, C.POINTER(Shape), i64, vp, i64, vp, i64, vp, vp, C.c_float, vp, vp, i32, i32, vp,
                                          vp, vp]
@@ -374,7 +379,7 @@ def fedattn_decode_noalloc(shape: Shape, mode: int, q, k_cache, v_cache, cache_s
                                        _ptr(lse), _stream(stream)), "fedattn_decode_noalloc")
 
 
-# ---- queries and keys before attention, and the 4-bit cache -------------------------------------------------------------
+# ---- windows, queries and keys before attention, and the 4-bit cache ---------------------------------------------------
 # These calls take tensors of several kinds; what the C call cannot see (types, shapes, strides) is checked here.
 def _stream_of(ctx: Context, stream) -> int:
     """The current stream of the context's device, which need not be the current device."""
@@ -407,6 +412,57 @@ def _rows(ctx: Context, t, n_rows: int, heads: int, shape: Shape, what: str):
     if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d) or (n_rows > 1 and t.stride(0) < heads * d):
         raise ValueError("%s: the heads of a row must be contiguous, and rows must not overlap" % what)
     return t.data_ptr(), t.stride(0) if n_rows > 1 else 0
+
+
+def _args_local_window(ctx, shape, q, k, v, cu_seqlens_host, window, n_sink, o, lse, stream):
+    if len(cu_seqlens_host) != shape.n_participants + 1:
+        raise ValueError("cu_seqlens must have N+1 entries")
+    L, hq, hkv, d, dt = int(q.shape[0]), shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.torch_dtype
+    if L != cu_seqlens_host[-1]:
+        raise ValueError("q has %d rows, the segments %d" % (L, cu_seqlens_host[-1]))
+    return (ctx.handle, C.byref(shape), _tensor(ctx, q, dt, (L, hq, d), "q"), _tensor(ctx, k, dt, (L, hkv, d), "k"),
+            _tensor(ctx, v, dt, (L, hkv, d), "v"), _i32_array(cu_seqlens_host), int(window), int(n_sink),
+            _tensor(ctx, o, dt, (L, hq, d), "o"), _tensor(ctx, lse, torch.float32, (L, hq), "lse"), _stream_of(ctx, stream))
+
+
+def fedattn_local_window(ctx: Context, shape: Shape, q, k, v, cu_seqlens_host: Sequence[int], window: int, n_sink: int, o,
+                         lse=None, stream=None):
+    """fedattn_local through a sliding window (|i - j| < window) with the segment's first n_sink rows always visible."""
+    _check(_lib.fedattn_local_window(*_args_local_window(ctx, shape, q, k, v, cu_seqlens_host, window, n_sink, o, lse, stream)),
+           "fedattn_local_window")
+
+
+def prepare_local_window(ctx: Context, shape: Shape, q, k, v, cu_seqlens_host: Sequence[int], window: int, n_sink: int, o,
+                         lse=None, stream=None):
+    return PreparedCall(_lib.fedattn_local_window,
+                        _args_local_window(ctx, shape, q, k, v, cu_seqlens_host, window, n_sink, o, lse, stream),
+                        "fedattn_local_window", (ctx, shape, q, k, v, o, lse))
+
+
+def _args_decode_window(ctx, shape, mode, q, k_cache, v_cache, cache_stride_participant, kv_len, max_kv_len, window, n_sink, o,
+                        lse, stream):
+    n, dt = shape.n_participants, shape.torch_dtype
+    rows = (n, shape.n_q_heads, shape.head_dim)
+    return (ctx.handle, C.byref(shape), int(mode), _tensor(ctx, q, dt, rows, "q"),
+            *[_tensor(ctx, t, dt, t.shape, "cache") for t in (k_cache, v_cache)], int(cache_stride_participant),
+            _tensor(ctx, kv_len, torch.int32, (1 if int(mode) == DECODE_SYNC else n,), "kv_len"), int(max_kv_len), int(window),
+            int(n_sink), _tensor(ctx, o, dt, rows, "o"), _tensor(ctx, lse, torch.float32, rows[:2], "lse"),
+            _stream_of(ctx, stream))
+
+
+def fedattn_decode_window(ctx: Context, shape: Shape, mode: int, q, k_cache, v_cache, cache_stride_participant: int, kv_len,
+                          max_kv_len: int, window: int, n_sink: int, o, lse=None, stream=None):
+    """fedattn_decode over the last `window` cached rows and the first n_sink."""
+    _check(_lib.fedattn_decode_window(*_args_decode_window(ctx, shape, mode, q, k_cache, v_cache, cache_stride_participant, kv_len,
+                                                           max_kv_len, window, n_sink, o, lse, stream)), "fedattn_decode_window")
+
+
+def prepare_decode_window(ctx: Context, shape: Shape, mode: int, q, k_cache, v_cache, cache_stride_participant: int, kv_len,
+                          max_kv_len: int, window: int, n_sink: int, o, lse=None, stream=None):
+    return PreparedCall(_lib.fedattn_decode_window,
+                        _args_decode_window(ctx, shape, mode, q, k_cache, v_cache, cache_stride_participant, kv_len, max_kv_len,
+                                            window, n_sink, o, lse, stream),
+                        "fedattn_decode_window", (ctx, shape, q, k_cache, v_cache, kv_len, o, lse))
 
 
 def _args_qk_norm_rope(ctx, shape, q, k, q_weight, k_weight, eps, pos, inv_freq, interleaved, q_out, k_out, stream):

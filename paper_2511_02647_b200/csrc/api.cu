@@ -81,6 +81,75 @@ struct DeviceGuard {
     ~DeviceGuard() { if (prev >= 0) status_of(cudaSetDevice(prev)); }
 };
 
+// window 0: the whole segment
+fedattn_status local_call(fedattn_ctx *ctx, const fedattn_shape *shape, const void *q, const void *k, const void *v, const int32_t *cu,
+                          int32_t window, int32_t n_sink, void *o, float *lse, fedattn_stream stream)
+{
+    if (!ctx || !shape_ok(shape) || !cu) return FEDATTN_ERR_INVALID_ARG;
+    const int N = shape->n_participants;
+    if (cu[0] != 0) return FEDATTN_ERR_INVALID_ARG;
+    for (int n = 0; n < N; ++n)
+        if (cu[n + 1] < cu[n]) return FEDATTN_ERR_INVALID_ARG;
+    const int64_t L = cu[N];
+    if (L == 0) return FEDATTN_OK;
+    if (!q || !k || !v || !o) return FEDATTN_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o)) return FEDATTN_ERR_INVALID_ARG;
+    DeviceGuard g(ctx->c.device);
+    if (g.err != cudaSuccess) return status_of(g.err);
+    PrefillParams p = prefill_params(shape, q, k, v, o, lse, L, L);
+    p.n_seg = N;
+    p.window = window; p.n_sink = n_sink;
+    memcpy(p.cu, cu, sizeof(int32_t) * (N + 1));
+    const cudaError_t err = launch_prefill(&ctx->c, p, shape->dtype, static_cast<cudaStream_t>(stream));
+    return status_of(err);
+}
+
+// window 0: every cached row
+fedattn_status decode_call(fedattn_ctx *ctx, const fedattn_shape *shape, int32_t mode, const void *q, const void *k_cache,
+                           const void *v_cache, int64_t cache_stride, const int32_t *kv_len, int32_t max_kv_len, int32_t window,
+                           int32_t n_sink, void *o, float *lse, fedattn_stream stream)
+{
+    if (!ctx || !shape_ok(shape)) return FEDATTN_ERR_INVALID_ARG;
+    if (mode != FEDATTN_DECODE_LOCAL && mode != FEDATTN_DECODE_SYNC) return FEDATTN_ERR_INVALID_ARG;
+    if (!q || !o || !kv_len || max_kv_len < 0 || cache_stride < 0) return FEDATTN_ERR_INVALID_ARG;
+    if (max_kv_len > 0 && (!k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache)))
+        return FEDATTN_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(o)) return FEDATTN_ERR_INVALID_ARG;
+    if (mode == FEDATTN_DECODE_LOCAL && (cache_stride * elt_bytes(shape)) % 16 != 0) return FEDATTN_ERR_INVALID_ARG;
+    DeviceGuard g(ctx->c.device);
+    if (g.err != cudaSuccess) return status_of(g.err);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    cudaError_t err;
+    const int N = shape->n_participants;
+    const size_t need = decode_scratch_bytes(N, shape->n_q_heads, shape->head_dim, ctx->c.sm_count);
+    if (shape->dtype == FEDATTN_BF16 && shape->head_dim == 128 && need > 0) {
+        if (ctx->c.scratch_bytes < need) return FEDATTN_ERR_WORKSPACE;
+        DecodeParams p;
+        memset(&p, 0, sizeof(p));
+        p.q = q; p.k = k_cache; p.v = v_cache; p.o = o; p.lse = lse;
+        p.n_part = N; p.hq = shape->n_q_heads; p.hkv = shape->n_kv_heads; p.d = shape->head_dim;
+        p.scale = eff_scale(shape); p.sync = mode == FEDATTN_DECODE_SYNC;
+        p.cache_stride = cache_stride; p.kv_len = kv_len; p.max_kv_len = max_kv_len;
+        p.window = window; p.n_sink = n_sink;
+        p.partial = reinterpret_cast<float *>(ctx->c.scratch); p.partial_bytes = ctx->c.scratch_bytes;
+        err = launch_decode_bf16(&ctx->c, p, s, &ctx->c.launches);
+    } else {
+        GenericParams p;
+        memset(&p, 0, sizeof(p));
+        p.q = q; p.k = k_cache; p.v = v_cache; p.o = o; p.lse = lse;
+        p.n_rows = N; p.hq = shape->n_q_heads; p.hkv = shape->n_kv_heads; p.d = shape->head_dim;
+        p.scale = eff_scale(shape); p.causal = 0;
+        p.mode = mode == FEDATTN_DECODE_SYNC ? kDecodeSync : kDecodeLocal;
+        p.kv_tok_stride = (int64_t)shape->n_kv_heads * shape->head_dim;
+        p.kv_head_stride = shape->head_dim;
+        p.kv_len = kv_len; p.cache_stride = cache_stride;
+        p.window = window; p.n_sink = n_sink;
+        err = launch_attn_generic(p, shape->dtype, max_kv_len, ctx->c.sm_count, s, &ctx->c.launches);
+        if (err == cudaSuccess) front_note(ctx->c.device, s, false);
+    }
+    return status_of(err);
+}
+
 }  // namespace
 
 extern "C" {
@@ -196,22 +265,14 @@ fedattn_status fedattn_poll(fedattn_ctx *ctx, fedattn_stream stream)
 fedattn_status fedattn_local(fedattn_ctx *ctx, const fedattn_shape *shape, const void *q, const void *k,
                              const void *v, const int32_t *cu, void *o, float *lse, fedattn_stream stream)
 {
-    if (!ctx || !shape_ok(shape) || !cu) return FEDATTN_ERR_INVALID_ARG;
-    const int N = shape->n_participants;
-    if (cu[0] != 0) return FEDATTN_ERR_INVALID_ARG;
-    for (int n = 0; n < N; ++n)
-        if (cu[n + 1] < cu[n]) return FEDATTN_ERR_INVALID_ARG;
-    const int64_t L = cu[N];
-    if (L == 0) return FEDATTN_OK;
-    if (!q || !k || !v || !o) return FEDATTN_ERR_INVALID_ARG;
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o)) return FEDATTN_ERR_INVALID_ARG;
-    DeviceGuard g(ctx->c.device);
-    if (g.err != cudaSuccess) return status_of(g.err);
-    PrefillParams p = prefill_params(shape, q, k, v, o, lse, L, L);
-    p.n_seg = N;
-    memcpy(p.cu, cu, sizeof(int32_t) * (N + 1));
-    const cudaError_t err = launch_prefill(&ctx->c, p, shape->dtype, static_cast<cudaStream_t>(stream));
-    return status_of(err);
+    return local_call(ctx, shape, q, k, v, cu, 0, 0, o, lse, stream);
+}
+
+fedattn_status fedattn_local_window(fedattn_ctx *ctx, const fedattn_shape *shape, const void *q, const void *k, const void *v,
+                                    const int32_t *cu, int32_t window, int32_t n_sink, void *o, float *lse, fedattn_stream stream)
+{
+    if (window < 1 || n_sink < 0) return FEDATTN_ERR_INVALID_ARG;
+    return local_call(ctx, shape, q, k, v, cu, window, n_sink, o, lse, stream);
 }
 
 fedattn_status fedattn_aggregate_kv(fedattn_ctx *ctx, const fedattn_shape *shape, int32_t mode,
@@ -350,43 +411,15 @@ fedattn_status fedattn_decode(fedattn_ctx *ctx, const fedattn_shape *shape, int3
                               const int32_t *kv_len, int32_t max_kv_len, void *o, float *lse,
                               fedattn_stream stream)
 {
-    if (!ctx || !shape_ok(shape)) return FEDATTN_ERR_INVALID_ARG;
-    if (mode != FEDATTN_DECODE_LOCAL && mode != FEDATTN_DECODE_SYNC) return FEDATTN_ERR_INVALID_ARG;
-    if (!q || !o || !kv_len || max_kv_len < 0 || cache_stride < 0) return FEDATTN_ERR_INVALID_ARG;
-    if (max_kv_len > 0 && (!k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache)))
-        return FEDATTN_ERR_INVALID_ARG;
-    if (!aligned16(q) || !aligned16(o)) return FEDATTN_ERR_INVALID_ARG;
-    if (mode == FEDATTN_DECODE_LOCAL && (cache_stride * elt_bytes(shape)) % 16 != 0) return FEDATTN_ERR_INVALID_ARG;
-    DeviceGuard g(ctx->c.device);
-    if (g.err != cudaSuccess) return status_of(g.err);
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    cudaError_t err;
-    const int N = shape->n_participants;
-    const size_t need = decode_scratch_bytes(N, shape->n_q_heads, shape->head_dim, ctx->c.sm_count);
-    if (shape->dtype == FEDATTN_BF16 && shape->head_dim == 128 && need > 0) {
-        if (ctx->c.scratch_bytes < need) return FEDATTN_ERR_WORKSPACE;
-        DecodeParams p;
-        memset(&p, 0, sizeof(p));
-        p.q = q; p.k = k_cache; p.v = v_cache; p.o = o; p.lse = lse;
-        p.n_part = N; p.hq = shape->n_q_heads; p.hkv = shape->n_kv_heads; p.d = shape->head_dim;
-        p.scale = eff_scale(shape); p.sync = mode == FEDATTN_DECODE_SYNC;
-        p.cache_stride = cache_stride; p.kv_len = kv_len; p.max_kv_len = max_kv_len;
-        p.partial = reinterpret_cast<float *>(ctx->c.scratch); p.partial_bytes = ctx->c.scratch_bytes;
-        err = launch_decode_bf16(&ctx->c, p, s, &ctx->c.launches);
-    } else {
-        GenericParams p;
-        memset(&p, 0, sizeof(p));
-        p.q = q; p.k = k_cache; p.v = v_cache; p.o = o; p.lse = lse;
-        p.n_rows = N; p.hq = shape->n_q_heads; p.hkv = shape->n_kv_heads; p.d = shape->head_dim;
-        p.scale = eff_scale(shape); p.causal = 0;
-        p.mode = mode == FEDATTN_DECODE_SYNC ? kDecodeSync : kDecodeLocal;
-        p.kv_tok_stride = (int64_t)shape->n_kv_heads * shape->head_dim;
-        p.kv_head_stride = shape->head_dim;
-        p.kv_len = kv_len; p.cache_stride = cache_stride;
-        err = launch_attn_generic(p, shape->dtype, max_kv_len, ctx->c.sm_count, s, &ctx->c.launches);
-        if (err == cudaSuccess) front_note(ctx->c.device, s, false);
-    }
-    return status_of(err);
+    return decode_call(ctx, shape, mode, q, k_cache, v_cache, cache_stride, kv_len, max_kv_len, 0, 0, o, lse, stream);
+}
+
+fedattn_status fedattn_decode_window(fedattn_ctx *ctx, const fedattn_shape *shape, int32_t mode, const void *q,
+                                     const void *k_cache, const void *v_cache, int64_t cache_stride, const int32_t *kv_len,
+                                     int32_t max_kv_len, int32_t window, int32_t n_sink, void *o, float *lse, fedattn_stream stream)
+{
+    if (window < 1 || n_sink < 0) return FEDATTN_ERR_INVALID_ARG;
+    return decode_call(ctx, shape, mode, q, k_cache, v_cache, cache_stride, kv_len, max_kv_len, window, n_sink, o, lse, stream);
 }
 
 fedattn_status fedattn_qk_norm_rope(fedattn_ctx *ctx, const fedattn_shape *shape, int64_t n_rows, const void *q,

@@ -96,7 +96,9 @@ template <typename T, int kR, int kDP, int kKeyWarps> struct Layout {
     static_assert(kKeyWarps * kM * kQPitch * 4 <= 2 * kKvBytes, "the partials take the place of the K and V tiles");
 };
 
-template <typename T, int kR, int kDP, int kKeyWarps>
+// kWindow: local and decode calls through a window.  The walk goes over the tiles with a sink, then over those from the first
+// row's window on.
+template <typename T, int kR, int kDP, int kKeyWarps, bool kWindow>
 __global__ void __launch_bounds__(Layout<T, kR, kDP, kKeyWarps>::kThreads)
 attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant__ TiledPlan plan)
 {
@@ -110,7 +112,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
     T *sKV = reinterpret_cast<T *>(smem + L::kOffKv);                        // [stage][K, V]
     float *part = reinterpret_cast<float *>(smem + L::kOffKv);               // [warp group][row][kQPitch], after the walk
     __shared__ float2 s_ml[kKeyWarps][kM];
-    __shared__ int s_bad[kM], s_last, s_lo[kM];
+    __shared__ int s_bad[kM], s_last, s_lo[kM], s_wl[kWindow ? kM : 1];
     __shared__ int64_t s_out[kM];                                            // stacked row -> row * hq + head
 
     namespace cg = cooperative_groups;
@@ -143,6 +145,19 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
     } else {
         kv_hi = (int)p.total_kv;
     }
+    int n_a = 0, t_b = 0, n_walk = 0, sink_end = 0;                          // tiles 0 .. n_a - 1, then t_b ..
+    if (kWindow) {
+        const int len = p.mode == kLocal ? p.cu[seg + 1] - kv_lo : kv_hi, token_n = token_of(n_rows - 1);
+        const bool causal = p.mode != kLocal || p.causal;
+        const WindowRule first(p.mode == kLocal ? token0 : len - 1, len, p.window, p.n_sink, causal);
+        const WindowRule last(p.mode == kLocal ? token_n : len - 1, len, p.window, p.n_sink, causal);
+        sink_end = kv_lo + (p.n_sink < len ? p.n_sink : len);
+        kv_hi = kv_lo + max(last.hi, last.sink);
+        n_a = last.sink > 0 ? (last.sink - 1) / kKeys + 1 : 0;
+        t_b = max(first.lo / kKeys, n_a);
+        n_walk = len > 0 ? n_a + max(0, (last.hi - 1) / kKeys + 1 - t_b) : 0;
+    }
+    auto tile_at = [&](int t) -> int { return !kWindow || t < n_a ? t : t_b + (t - n_a); };
     const int64_t kv_base = (int64_t)kvh * p.kv_head_stride + (p.mode == kDecodeLocal ? (int64_t)seg * p.cache_stride : 0);
     const T *K = reinterpret_cast<const T *>(p.k) + kv_base, *V = reinterpret_cast<const T *>(p.v) + kv_base;
     const int32_t *kvp = p.kv_pos ? p.kv_pos + (int64_t)kvh * p.kv_pos_head_stride : nullptr;
@@ -167,13 +182,13 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
     };
     // the first K and V tile are on their way while Q and the rows' bounds are set up (a walk that turns out shorter
     // does not use them)
-    const int n_kt_most = kv_hi > kv_lo ? (kv_hi - kv_lo - 1) / kKeys + 1 : 0;
+    const int n_kt_most = kWindow ? n_walk : (kv_hi > kv_lo ? (kv_hi - kv_lo - 1) / kKeys + 1 : 0);
     constexpr int kKvElts = L::kKvBytes / (int)sizeof(T);
     const int stages = plan.stages;
 #pragma unroll 1
     for (int x = 0; x < 2 * stages; ++x) {
         const int t = rank + (x >> 1) * plan.splits;
-        if (t < n_kt_most) load_tile(sKV + x * kKvElts, (x & 1) ? V : K, t);
+        if (t < n_kt_most) load_tile(sKV + x * kKvElts, (x & 1) ? V : K, tile_at(t));
         else asm volatile("cp.async.commit_group;" ::: "memory");
     }
 
@@ -185,6 +200,12 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
         if (r >= n_rows) lo = INT_MIN;                                       // no such row
         else if (p.mode == kLocal && p.causal) lo = row;
         else if (by_pos) lo = p.remote_only ? p.cu[seg] - 1 : (p.q_pos ? ld_int(p.q_pos + row) : row);
+        if (kWindow) {
+            const int len = p.mode == kLocal ? p.cu[seg + 1] - kv_lo : kv_hi;
+            const WindowRule w(p.mode == kLocal ? tok : len - 1, len, p.window, p.n_sink, p.mode != kLocal || p.causal);
+            if (r < n_rows) lo = kv_lo + w.hi - 1;
+            s_wl[r] = r < n_rows ? kv_lo + w.lo : INT_MIN;
+        }
         s_lo[r] = lo;
         s_bad[r] = 0;
     }
@@ -198,10 +219,16 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
         if (r < n_rows) v = lds4(reinterpret_cast<const T *>(p.q) + s_out[r] * d + c);
         *reinterpret_cast<float4 *>(sQ + r * L::kQPitch + c) = v;
     }
-    int lo[kR], lo_max = INT_MIN, lo_min = INT_MAX;
+    int lo[kR], wl[kWindow ? kR : 1], lo_max = INT_MIN, lo_min = INT_MAX, wl_max = INT_MIN;
     const int my_row0 = ((kKeyWarps > 1 ? 0 : 2 * warp) + half) * kR;
 #pragma unroll
     for (int i = 0; i < kR; ++i) lo[i] = s_lo[my_row0 + i];
+    if (kWindow) {
+#pragma unroll
+        for (int i = 0; i < kR; ++i) wl[i] = s_wl[my_row0 + i];
+        for (int r = lane; r < n_rows; r += 32) wl_max = max(wl_max, s_wl[r]);
+        wl_max = __reduce_max_sync(0xffffffffu, wl_max);
+    }
     for (int r = lane; r < n_rows; r += 32) { lo_max = max(lo_max, s_lo[r]); lo_min = min(lo_min, s_lo[r]); }
     lo_max = __reduce_max_sync(0xffffffffu, lo_max);
     lo_min = __reduce_min_sync(0xffffffffu, lo_min);
@@ -231,7 +258,8 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
         }
     }
 
-    const int n_kt = kv_hi > kv_lo ? (kv_hi - kv_lo - 1) / kKeys + 1 : 0;
+    const int n_kt = kWindow ? n_walk : (kv_hi > kv_lo ? (kv_hi - kv_lo - 1) / kKeys + 1 : 0);
+    const bool causal = p.mode != kLocal || p.causal;
     float m[kR], l[kR];
     uint64_t acc[kR / 2][kC];                                                // rows (2 i, 2 i + 1)
 #pragma unroll
@@ -257,10 +285,10 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
             pos[j] = kvp && by_pos ? ld_int(kvp + key) : key;
         }
     };
-    if (rank < n_kt) load_pos(rank);
+    if (rank < n_kt) load_pos(tile_at(rank));
 #pragma unroll 1
     for (int t = rank; t < n_kt; t += plan.splits) {
-        const int k0 = kv_lo + t * kKeys, left = kv_hi - k0;                 // keys from the tile's first to the last
+        const int k0 = kv_lo + tile_at(t) * kKeys, left = kv_hi - k0;        // keys from the tile's first to the last
         const int next = t + stages * plan.splits;                           // the tile that takes this one's place
         T *sK = sKV + 2 * slot * kKvElts, *sV = sK + kKvElts;
         slot = slot + 1 == stages ? 0 : slot + 1;
@@ -290,10 +318,10 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
             }
         }
         __syncthreads();                                                     // every warp is done with K
-        if (next < n_kt) load_tile(sK, K, next);
+        if (next < n_kt) load_tile(sK, K, tile_at(next));
         else asm volatile("cp.async.commit_group;" ::: "memory");
         // ---- mask, online softmax (16 lanes share a row), P transposed to shared memory ----
-        const bool all_seen = !(kvp && by_pos) && !two_sided && kKeys <= left && k0 + kKeys - 1 <= lo_min;
+        const bool all_seen = !(kvp && by_pos) && !two_sided && kKeys <= left && k0 + kKeys - 1 <= lo_min && (!kWindow || k0 >= wl_max);
         float al[kR];
 #pragma unroll
         for (int i = 0; i < kR; ++i) {
@@ -302,7 +330,11 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
             for (int j = 0; j < kJ; ++j) {
                 const float2 v = unpack2(s2[i][j]);
                 s[j] = (v.x + v.y) * p.scale;
-                if (!all_seen && !(key_l + 16 * j < left && (pos[j] <= lo[i] || (two_sided && pos[j] >= hi && my_row0 + i < n_rows))))
+                if (kWindow) {
+                    // (a sink that a causal row stands before lies behind its last key)
+                    const bool seen = key_l + 16 * j < left && ((pos[j] <= lo[i] && pos[j] >= wl[i]) || (pos[j] < sink_end && (!causal || pos[j] <= lo[i])));
+                    if (!all_seen && !seen) s[j] = -INFINITY;
+                } else if (!all_seen && !(key_l + 16 * j < left && (pos[j] <= lo[i] || (two_sided && pos[j] >= hi && my_row0 + i < n_rows))))
                     s[j] = -INFINITY;
                 mx = fmaxf(mx, s[j]);
             }
@@ -335,7 +367,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
 #pragma unroll
             for (int c = 0; c < kC; ++c) acc[i][c] = mul2(acc[i][c], a2);
         }
-        if (t + plan.splits < n_kt) load_pos(t + plan.splits);
+        if (t + plan.splits < n_kt) load_pos(tile_at(t + plan.splits));
         wait_copy();                                                         // V
         // ---- O += P V ----
         const int kb = kKeyWarps > 1 ? 16 * warp : 0;
@@ -358,7 +390,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
             }
         }
         __syncthreads();                                                     // every warp is done with V (and P)
-        if (next < n_kt) load_tile(sV, V, next);
+        if (next < n_kt) load_tile(sV, V, tile_at(next));
         else asm volatile("cp.async.commit_group;" ::: "memory");
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -431,8 +463,8 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
     if (plan.splits > 1) cluster.sync();                                     // peers may still be reading this CTA's partials
 }
 
-template <typename T, int kR, int kDP, int kKeyWarps>
-cudaError_t launch_variant(const GenericParams &p, TiledPlan plan, int sm_count, int64_t max_kv, cudaStream_t s)
+template <typename T, int kR, int kDP, int kKeyWarps, bool kWindow>
+cudaError_t launch_instance(const GenericParams &p, TiledPlan plan, int sm_count, int64_t max_kv, cudaStream_t s)
 {
     using L = Layout<T, kR, kDP, kKeyWarps>;
     constexpr int kMost = 110 * 1024;                                        // two CTAs per SM (a cluster of 8 finds few places among
@@ -450,7 +482,7 @@ cudaError_t launch_variant(const GenericParams &p, TiledPlan plan, int sm_count,
     cudaError_t e = cudaGetDevice(&dev);
     static bool attr_set[64] = {};                                           // the attribute is per device
     if (e == cudaSuccess && !attr_set[dev & 63]) {
-        e = cudaFuncSetAttribute(attn_tiled_kernel<T, kR, kDP, kKeyWarps>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+        e = cudaFuncSetAttribute(attn_tiled_kernel<T, kR, kDP, kKeyWarps, kWindow>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
         attr_set[dev & 63] = e == cudaSuccess;
     }
     if (e != cudaSuccess) return e;
@@ -458,7 +490,18 @@ cudaError_t launch_variant(const GenericParams &p, TiledPlan plan, int sm_count,
     l.attr[1].id = cudaLaunchAttributeClusterDimension;
     l.attr[1].val.clusterDim.x = plan.splits; l.attr[1].val.clusterDim.y = 1; l.attr[1].val.clusterDim.z = 1;
     l.cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&l.cfg, attn_tiled_kernel<T, kR, kDP, kKeyWarps>, p, plan);
+    return cudaLaunchKernelEx(&l.cfg, attn_tiled_kernel<T, kR, kDP, kKeyWarps, kWindow>, p, plan);
+}
+
+template <typename T, int kR, int kDP, int kKeyWarps>
+cudaError_t launch_variant(const GenericParams &p, const TiledPlan &plan, int sm_count, int64_t max_kv, cudaStream_t s)
+{
+    if (p.window > 0) {
+        // tiles with a sink, those of a row tile's windows, and what the ends of both cut off
+        const int64_t most = (int64_t)p.n_sink + p.window + (p.mode == kLocal && !p.causal ? p.window : 0) + 4 * Layout<T, kR, kDP, kKeyWarps>::kKeys;
+        return launch_instance<T, kR, kDP, kKeyWarps, true>(p, plan, sm_count, most < max_kv ? most : max_kv, s);
+    }
+    return launch_instance<T, kR, kDP, kKeyWarps, false>(p, plan, sm_count, max_kv, s);
 }
 
 // M = 8, 16 (keys over warps), 32 (rows over warps; four CTAs of 64 channels share an SM.  64 rows at 8 per thread

@@ -66,6 +66,21 @@ __device__ __noinline__ void attn_row_warp(const GenericParams &p, int64_t row, 
         kv_hi = p.kv_len[0];
         test_pos = false;
     }
+    int64_t win_lo = 0, win_hi = kv_hi, sink_hi = 0; // through a window: [win_lo, win_hi) and [kv_lo, sink_hi)
+    if (p.window > 0) {
+        const int n_keys = (int)(kv_hi - kv_lo);
+        int i = n_keys - 1, len = n_keys;
+        bool causal = true;
+        if (p.mode == kLocal) {
+            int n = 0;
+            while (n + 1 < p.n_seg && row >= p.cu[n + 1]) ++n;
+            i = (int)(row - p.cu[n]);
+            len = p.cu[n + 1] - p.cu[n];
+            causal = p.causal != 0;
+        }
+        const WindowRule w(i, len, p.window, p.n_sink, causal);
+        win_lo = kv_lo + w.lo; win_hi = kv_lo + w.hi; sink_hi = kv_lo + w.sink;
+    }
     const T *K = reinterpret_cast<const T *>(p.k) + kv_base;
     const T *V = reinterpret_cast<const T *>(p.v) + kv_base;
     const int32_t *kvp = p.kv_pos ? p.kv_pos + (int64_t)kvh * p.kv_pos_head_stride : nullptr;
@@ -88,6 +103,7 @@ __device__ __noinline__ void attn_row_warp(const GenericParams &p, int64_t row, 
             const int64_t pj = kvp ? kvp[j] : j;
             ok = pj < own_lo || pj >= own_hi;
         }
+        if (p.window > 0) ok = ok && ((j >= win_lo && j < win_hi) || j < sink_hi);
         float s = -INFINITY;
         if (ok) {
             const T *kr = K + j * p.kv_tok_stride;

@@ -146,8 +146,23 @@ struct GenericParams {
     const int32_t *kv_pos;        // nullable
     const int32_t *kv_len;        // decode: dev lengths
     int64_t cache_stride;         // decode local: elements between participants' caches
+    int32_t window, n_sink;       // local, decode: window > 0: see WindowRule
     int32_t n_seg;
     int32_t cu[kMaxP + 1];        // local: segment offsets
+};
+// Which keys of its segment (or cache) of `len` rows row i sees through a window: those at a distance below `window`, not behind it
+// when causal, and the first n_sink (causal: as far as they are not behind it): [lo, hi) and [0, sink).  A decode row stands at
+// len - 1 (the last cached row), causal.
+struct WindowRule {
+    int lo, hi, sink;
+    __host__ __device__ WindowRule(int i, int len, int window, int n_sink, bool causal)
+    {
+        lo = i >= window ? i - window + 1 : 0;
+        hi = causal ? i + 1 : (len - i > window ? i + window : len);
+        const int most = causal ? i + 1 : len;
+        sink = n_sink < most ? n_sink : most;
+    }
+    __device__ bool sees(int x) const { return (x >= lo && x < hi) || x < sink; }
 };
 
 // max_kv: an upper bound (decode: the caller's) on the keys of one row, which only sets how many CTAs share them
@@ -189,6 +204,7 @@ struct PrefillParams {
     int32_t general;              // sync, causal: every (query, key) pair is tested on explicit positions
     const int32_t *q_pos;         // general: nullable (= row index)
     int32_t *tab;                 // general: scratch for the position tables (position_table_bytes)
+    int32_t window, n_sink;       // local: window > 0: see WindowRule
     int32_t n_seg;
     int32_t cu[kMaxP + 1];        // query segments (local: also the KV segments)
 };
@@ -203,6 +219,7 @@ inline GenericParams generic_params(const PrefillParams &p)
     g.kv_head_stride = p.kv_head_major ? p.total_kv * p.d : p.d;
     g.kv_pos_head_stride = p.kv_head_major ? p.total_kv : 0;
     g.total_kv = p.total_kv; g.q_pos = p.q_pos; g.kv_pos = p.kv_pos;
+    g.window = p.window; g.n_sink = p.n_sink;
     g.n_seg = p.n_seg;
     for (int i = 0; i <= p.n_seg; ++i) g.cu[i] = p.cu[i];
     return g;
@@ -231,6 +248,7 @@ struct DecodeParams {
     int64_t cache_stride;
     const int32_t *kv_len;
     int32_t max_kv_len;
+    int32_t window, n_sink;       // window 0: every key
     float *partial;               // scratch: per-split partial results
     size_t partial_bytes;
     int32_t g_shift;              // log2(hq / hkv) when that is a power of two, else -1 (set by the launcher)

@@ -128,7 +128,8 @@ __device__ long long g_dtrace[1024 * 8];
 // = { m (log2 domain, scale included), l, -, -, o[128] }, unnormalised.
 // kOneLaunch: the grid's x extent is one cluster; warps leave their partials in shared memory, every CTA folds its
 // slices, and rank r of the cluster folds and writes rows r, r + n_splits, ...
-template <int kMTiles, bool kOneLaunch>
+// kWindow: the first n_sink and the last `window` keys only: the walk goes over tiles 0 .. n_a - 1, then t_b and on.
+template <int kMTiles, bool kOneLaunch, bool kWindow>
 __global__ void __launch_bounds__(128, 2)
 decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
 {
@@ -148,7 +149,16 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
     const int rows_total = p.sync ? p.n_part * g : g;          // query rows sharing this cache + KV head
 
     const int len = p.sync ? p.kv_len[0] : p.kv_len[cache];
-    const int tiles_total = (len + kTileKeys - 1) / kTileKeys;
+    int tiles_total = (len + kTileKeys - 1) / kTileKeys;
+    int n_a = 0, t_b = 0, win_lo = 0, sink = 0;
+    if (kWindow && len > 0) {
+        const WindowRule w(len - 1, len, p.window, p.n_sink, true);
+        win_lo = w.lo; sink = w.sink;
+        n_a = (sink + kTileKeys - 1) / kTileKeys;
+        t_b = max(win_lo / kTileKeys, n_a);
+        tiles_total = n_a + (tiles_total - t_b);
+    }
+    auto key0_of = [&](int tile) -> int { return (!kWindow || tile < n_a ? tile : t_b + (tile - n_a)) * kTileKeys; };
     const int tiles_per_split = (tiles_total + n_splits - 1) / n_splits;
     const int tile_lo = min(split * tiles_per_split, tiles_total);
     const int tile_hi = min(tile_lo + tiles_per_split, tiles_total);
@@ -179,7 +189,7 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
     const __nv_bfloat16 *ld_k = Kb + (size_t)ld_row * tok_stride + ld_ch * 8, *ld_v = Vb + (size_t)ld_row * tok_stride + ld_ch * 8;
     const uint32_t ld_s = smem_u32(smem) + swz(ld_row, ld_ch);
     auto load_tile = [&](int t, int stage) {
-        const int key0 = (tile_lo + t) * kTileKeys;
+        const int key0 = key0_of(tile_lo + t);
         const uint32_t sK = ld_s + stage * kStageBytes, sV = sK + kTileBytes;
         const size_t base = (size_t)key0 * tok_stride;
         const int n_ok = len - key0 - ld_row;                  // rows ld_row + 8 i with 8 i < n_ok exist
@@ -254,8 +264,9 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
                 mma_bf16(s1, qf[ks], b[2], b[3]);
             }
             // ---- mask keys past the end, online softmax (rows lane/4 and lane/4+8) ----
-            const int key = (tile_lo + t) * kTileKeys + krow0 + (lane & 3) * 2;
-            const bool ok[4] = {key < len, key + 1 < len, key + 8 < len, key + 9 < len};
+            const int key = key0_of(tile_lo + t) + krow0 + (lane & 3) * 2;
+            auto seen = [&](int x) -> bool { return x < len && (!kWindow || x >= win_lo || x < sink); };
+            const bool ok[4] = {seen(key), seen(key + 1), seen(key + 8), seen(key + 9)};
             float v[8] = {s0[0], s0[1], s1[0], s1[1], s0[2], s0[3], s1[2], s1[3]};   // row0: v[0..3], row1: v[4..7]
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -497,7 +508,18 @@ size_t decode_scratch_bytes(int n_part, int hq, int d, int /*sm_count*/)
     return (size_t)n_part * hq * kMaxSlots * kPartialStride * sizeof(float);
 }
 
-// Grid rule shared by both entry points.  Splits are chosen so that the whole stream grid is resident
+typedef void (*StreamKernel)(const DecodeParams, int, int);
+static StreamKernel stream_kernel(int m_tiles, bool one_launch, bool window)
+{
+    static const StreamKernel kernels[2][2][2] = {
+        {{decode_stream_kernel<1, false, false>, decode_stream_kernel<1, false, true>},
+         {decode_stream_kernel<1, true, false>, decode_stream_kernel<1, true, true>}},
+        {{decode_stream_kernel<2, false, false>, decode_stream_kernel<2, false, true>},
+         {decode_stream_kernel<2, true, false>, decode_stream_kernel<2, true, true>}}};
+    return kernels[m_tiles - 1][one_launch][window];
+}
+
+// Grid rule shared by the entry points.  Splits are chosen so that the whole stream grid is resident
 // at once (two CTAs per SM): a grid slightly larger than that would run a nearly empty second wave.
 static cudaError_t launch_decode_split(const DecodeParams &p_in, int device, int sm_count, cudaStream_t s,
                                        int64_t *launches)
@@ -525,7 +547,10 @@ static cudaError_t launch_decode_split(const DecodeParams &p_in, int device, int
     const int n_chunks = (rows_total + 16 * m_tiles - 1) / (16 * m_tiles);
     const int caches = p.sync ? 1 : p.n_part;
     const int sources = caches * p.hkv * n_chunks;
-    const int tiles = (p.max_kv_len + kTileKeys - 1) / kTileKeys;
+    // keys that a walk goes over, at most
+    int64_t keys = p.max_kv_len;
+    if (p.window > 0 && (int64_t)p.window + p.n_sink + 2 * kTileKeys < keys) keys = (int64_t)p.window + p.n_sink + 2 * kTileKeys;
+    const int tiles = (int)((keys + kTileKeys - 1) / kTileKeys);
     int n_splits = 2 * sm_count / sources;                     // rounded down: one wave
     if (n_splits > tiles / 2) n_splits = tiles / 2;            // at least two tiles per split
     if (n_splits > kMaxSlots / slices) n_splits = kMaxSlots / slices;
@@ -534,7 +559,7 @@ static cudaError_t launch_decode_split(const DecodeParams &p_in, int device, int
     // 32 splits take 12 us, 8 take 31); two CTAs per SM hold a cluster of 8 everywhere.
     int cluster = 1;
     while (cluster * 2 <= n_splits && cluster < kMaxCluster) cluster *= 2;
-    const bool one_launch = (int64_t)caches * p.hkv * p.max_kv_len * kD * 4 <= kOneLaunchBytes && tiles <= kOneLaunchTiles * cluster;
+    const bool one_launch = caches * p.hkv * keys * kD * 4 <= kOneLaunchBytes && tiles <= kOneLaunchTiles * cluster;
     if (one_launch) n_splits = cluster;
     const int n_slots = n_splits * slices;
     if (!one_launch && (size_t)p.n_part * p.hq * n_slots * kPartialStride * sizeof(float) > p.partial_bytes)
@@ -552,13 +577,7 @@ static cudaError_t launch_decode_split(const DecodeParams &p_in, int device, int
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = one_launch ? 2 : 1;
-    cudaError_t e;
-    if (one_launch)
-        e = m_tiles == 1 ? cudaLaunchKernelEx(&cfg, decode_stream_kernel<1, true>, p, n_splits, n_chunks)
-                         : cudaLaunchKernelEx(&cfg, decode_stream_kernel<2, true>, p, n_splits, n_chunks);
-    else
-        e = m_tiles == 1 ? cudaLaunchKernelEx(&cfg, decode_stream_kernel<1, false>, p, n_splits, n_chunks)
-                         : cudaLaunchKernelEx(&cfg, decode_stream_kernel<2, false>, p, n_splits, n_chunks);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, stream_kernel(m_tiles, one_launch, p.window > 0), p, n_splits, n_chunks);
     if (launches) ++*launches;
     if (one_launch) return early_start_end(es, e != cudaSuccess ? e : cudaGetLastError());
     cfg.numAttrs = 1;
@@ -576,10 +595,9 @@ static cudaError_t set_decode_smem_attr()
 {
     const int smem = kStages * kStageBytes;
     cudaError_t e = cudaSuccess;
-    void (*const kernels[])(const DecodeParams, int, int) = {decode_stream_kernel<1, false>, decode_stream_kernel<2, false>,
-                                                             decode_stream_kernel<1, true>, decode_stream_kernel<2, true>};
-    for (auto k : kernels)
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    for (int i = 0; i < 8; ++i)
+        if (e == cudaSuccess)
+            e = cudaFuncSetAttribute(stream_kernel(1 + (i & 1), i & 2, i & 4), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     return e;
 }
 

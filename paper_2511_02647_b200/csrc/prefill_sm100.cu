@@ -427,7 +427,7 @@ struct Sub {
 struct Item {
     int kvh, seg, kv_begin;
     // The walk visits KV tiles 0 .. n_a-1 and then t_b0, t_b0+1, ...  (n_a == n_tiles unless the allowed
-    // keys are two ranges: bidirectional remote-only attention, keys [0, a) and [b, T)).
+    // keys are two ranges: bidirectional remote-only attention, keys [0, a) and [b, T); a window and its sinks).
     int n_a, t_b0, a, b;
     const int32_t *kvp;                // positions of this KV head's aggregated rows (sparse sync), or null
 };
@@ -497,7 +497,8 @@ __device__ __forceinline__ int last_visible_tile(const KernelParams &kp, const I
 // Called by a converged warp (all lanes get the same item).  kSpecial: the kernel instance that also
 // serves explicit positions and bidirectional remote-only attention (two key ranges); the plain instance
 // carries none of their state.  Causal remote-only attention is one more prefix mask: plain instance.
-template <bool kSpecial, bool kExact, bool kHalves, int kKeys>
+// kWindow: local attention through a window.
+template <bool kSpecial, bool kExact, bool kHalves, bool kWindow, int kKeys>
 __device__ __forceinline__ Item decode_item(const KernelParams &kp, int item, int lane, Sub (&sub)[2], uint16_t *walk)
 {
     const PrefillParams &p = kp.p;
@@ -595,6 +596,20 @@ __device__ __forceinline__ Item decode_item(const KernelParams &kp, int item, in
             sub[1].n_tiles = it.n_a + (n_t - it.t_b0);
         }
         sub[0].n_tiles = sub[0].n_valid > 0 ? sub[1].n_tiles : 0;
+    } else if (kWindow) {
+        // the tiles with a sink, then those from the first row's window to the last row's; both sub-tiles walk what either may see
+        int lo_row = sub[1].q_row0, hi_row = sub[1].q_row0 + sub[1].n_valid - 1;
+        if (two_rows && sub[0].n_valid > 0) {
+            lo_row = min(lo_row, sub[0].q_row0);
+            hi_row = max(hi_row, sub[0].q_row0 + sub[0].n_valid - 1);
+        }
+        const int len = end - p.cu[seg];
+        const WindowRule first(lo_row - p.cu[seg], len, p.window, p.n_sink, p.causal != 0);
+        const WindowRule last(hi_row - p.cu[seg], len, p.window, p.n_sink, p.causal != 0);
+        it.n_a = (last.sink + kKeys - 1) / kKeys;
+        it.t_b0 = max(first.lo / kKeys, it.n_a);
+        sub[1].n_tiles = it.n_a + max(0, (last.hi + kKeys - 1) / kKeys - it.t_b0);
+        sub[0].n_tiles = sub[0].n_valid > 0 ? sub[1].n_tiles : 0;
     } else {
         // (one copy of the searches' code, walked a second time when the sub-tiles are different query tiles)
 #pragma unroll 1
@@ -637,7 +652,11 @@ __device__ __forceinline__ Item decode_item(const KernelParams &kp, int item, in
 // maximum and sum go through shared memory).  An item takes half as long as a pair of heads over the same keys: for
 // launches whose longest walk, not their sum of work, decides.  K and V tiles then serve one product each, which
 // doubles what the CTA reads from L2.
-template <bool kSpecial, int kBoxes, bool kExact, bool kHalves>
+//
+// kWindow: local attention through a window, with sinks.  Two key ranges per row, [lo, hi) and [0, sink), whose masks are four more bit
+// operations per word of a partial tile; tiles between the sinks and the first row's window are never loaded.  Every exponential is ex2: a
+// walk is a few tiles, and the polynomial's 7.5e-5 would be most of what lse is off by.
+template <bool kSpecial, int kBoxes, bool kExact, bool kHalves, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_o,
@@ -737,7 +756,7 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const bool general = kSpecial && !kExact && p.general;
             if (general && !slot_free()) break;                 // the walk goes into the slot while decoding
             uint16_t *walk = walks + (pn & 1) * kWalkMost;
-            const Item it = decode_item<kSpecial, kExact, kHalves, kKeys>(kp, item, lane, sub, walk);
+            const Item it = decode_item<kSpecial, kExact, kHalves, kWindow, kKeys>(kp, item, lane, sub, walk);
             __syncwarp();
             const int n_tiles = sub[1].n_tiles + (kHalves ? sub[0].n_tiles : 0);
             if (!general && !slot_free()) break;
@@ -777,7 +796,7 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 const bool listed = general && it.b < 0;
                 for (int j = 0; j < n_tiles; ++j) {
                     const int gt = git + j, st = gt & 1, use = gt >> 1;
-                    int tile = kSpecial ? tile_of(it, j) : j;
+                    int tile = kSpecial || kWindow ? tile_of(it, j) : j;
                     if (listed) tile = walk[j] & 0x7fff;
                     const int row = it.kv_begin + tile * kKeys;
                     const int c1 = p.kv_head_major ? row : it.kvh, c2 = p.kv_head_major ? it.kvh : row;
@@ -951,7 +970,7 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         // every exponential goes through ex2.approx, which maps -inf to 0; in unmasked tiles a fixed subset of
         // the columns takes the polynomial so that the ex2 unit is not the bottleneck.
         // kAnyFirst: the tile in which a row sees its first key may be any of the walk (explicit positions).
-        constexpr bool kAnyFirst = kSpecial || kExact;
+        constexpr bool kAnyFirst = kSpecial || kExact || kWindow;
         auto visit = [&](auto partial_tag, int j, int gt, const uint32_t (&vm)[4], float &m_used, float &l) {
             constexpr bool kPartial = decltype(partial_tag)::value;
             mbar_wait(s_full + t, gt & 1, abort_flag, kp.status);
@@ -1036,7 +1055,7 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 for (int i = 0; i < 16; ++i) {
                     const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(cur[2 * i]), __uint_as_float(cur[2 * i + 1])), sl2_2, negm2);
                     float p0, p1;
-                    if (!kExact && !kPartial && ((kPolyMask >> (i & 7)) & 1)) {
+                    if (!kExact && !kWindow && !kPartial && ((kPolyMask >> (i & 7)) & 1)) {
                         exp2_poly_x2(x2, p0, p1);
                     } else {
                         float x0, x1;
@@ -1114,6 +1133,8 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const bool pairs = kExact && kp.pairs;
             int c_row = 0, n_full = 0, p_row = 0;
             PairRule mine{0, 0, false}, all{0, 0, false};       // pairs: this row's rule, and what every row of the warp sees
+            int w_lo = 0, w_hi = 0, w_sink = 0;                 // window: what this row sees, from the segment's start
+            int all_lo = 0, all_hi = 0, all_sink = 0;           // and what every row of the warp sees
             int kpos[4] = {0, 0, 0, 0};                         // pairs: positions of keys 32 c + lane of the tile at hand
             auto load_pos = [&](int j) {
                 const int T = (int)p.total_kv;
@@ -1128,6 +1149,14 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 all = mine;
                 all.lo = __reduce_min_sync(0xffffffffu, mine.lo);
                 load_pos(kHalves ? 1 - t : 0);
+            } else if (kWindow) {
+                // (rows that do not exist take the last one's; both ends grow with the row)
+                const int i = sub.q_row0 + min(r, sub.n_valid - 1) - p.cu[it.seg];
+                const WindowRule w(i, p.cu[it.seg + 1] - p.cu[it.seg], p.window, p.n_sink, p.causal != 0);
+                w_lo = w.lo; w_hi = w.hi; w_sink = w.sink;
+                all_lo = __shfl_sync(0xffffffffu, w.lo, 31);
+                all_hi = __shfl_sync(0xffffffffu, w.hi, 0);
+                all_sink = __shfl_sync(0xffffffffu, w.sink, 0);
             } else if (general) {
                 // every (query, key) pair on its own positions
                 n_full = it.b;
@@ -1185,6 +1214,16 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         }
                     }
                     if (j + 1 < n_tiles) load_pos(tile + (kHalves ? 2 : 1));        // lands during this tile's visit
+                } else if (kWindow) {
+                    const int k0 = tile_of(it, tile) * kKeys;
+                    full = (k0 >= all_lo && k0 + kKeys <= all_hi) || k0 + kKeys <= all_sink;
+                    if (!full) {
+#pragma unroll
+                        for (int c = 0; c < kChunks; ++c) {
+                            const int cb = k0 + 32 * c;
+                            vm[c] = (below32(w_hi - cb) & ~below32(w_lo - cb)) | below32(w_sink - cb);
+                        }
+                    }
                 } else if (two_range) {                         // keys [0, a) and [b, T)
                     const int k0 = tile_of(it, tile) * kKeys;   // first key of the tile
                     full = k0 + kKeys <= it.a || (k0 >= it.b && k0 + kKeys <= T);
@@ -1394,7 +1433,7 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             // (halves: sub-tile 1's warpgroup, which has a part in every item, writes it)
             if (valid && lse_p && !(kHalves && halved && t == 0) && !((bad >> lane) & 1u))
-                *lse_p = !(l_run > 0.f) ? -INFINITY : kExact ? lse_exact(m_run, l_run) : (m_run + log2f(l_run)) * 0.6931471805599453f;
+                *lse_p = !(l_run > 0.f) ? -INFINITY : kExact || kWindow ? lse_exact(m_run, l_run) : (m_run + log2f(l_run)) * 0.6931471805599453f;
             if (kExact && bad && !(kHalves && halved && t == 0)) {      // (one warpgroup redoes them, neither stores them)
                 if (lane == 0) tma_store_wait_read();           // the staging rows are free again: the routine's row of Q
                 __syncwarp();
@@ -1575,7 +1614,11 @@ static ItemForm item_form(const PrefillParams &p, int64_t n_qtiles, int sm_count
     auto walk = [&](int seg, int tile, int tiles) -> float {
         if (p.remote_only) return p.causal ? n_kt * p.cu[seg] / p.n_q_rows : n_kt;
         const float most = p.sync ? n_kt : (float)tiles;
-        return grows ? most * tile / tiles : most;
+        const float all = grows ? most * tile / tiles : most;
+        if (p.window == 0) return all;
+        // the rows' own tile, the window before (and behind) it, the sinks
+        const float seen = 1.f + (p.causal ? 1.f : 2.f) * ((float)p.window / kTileN) + (p.n_sink > 0 ? 1.f + (float)(p.n_sink / kTileN) : 0.f);
+        return seen < all ? seen : all;
     };
     auto tiles_of = [&](int seg) { return (p.cu[seg + 1] - p.cu[seg] + kTileM - 1) / kTileM; };
     if (n_qtiles * p.hkv * ((g + 1) / 2) > 3 * sm_count) {
@@ -1699,15 +1742,18 @@ cudaError_t launch_prefill_sm100(Context *ctx, const PrefillParams &p, cudaStrea
     // and bidirectional remote-only attention run the instance that carries their extra state; head dims below
     // 128 run the exact instances
     typedef void (*Kernel)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const KernelParams);
-    static const Kernel kernels[8] = {
-        prefill_sm100_kernel<false, 2, false, false>, prefill_sm100_kernel<true, 2, false, false>,
-        prefill_sm100_kernel<true, 1, true, false>,   prefill_sm100_kernel<true, 2, true, false>,
-        prefill_sm100_kernel<false, 2, false, true>,  prefill_sm100_kernel<true, 2, false, true>,
-        prefill_sm100_kernel<true, 1, true, true>,    prefill_sm100_kernel<true, 2, true, true>};
+    static const Kernel kernels[14] = {
+        prefill_sm100_kernel<false, 2, false, false, false>, prefill_sm100_kernel<true, 2, false, false, false>,
+        prefill_sm100_kernel<true, 1, true, false, false>,   prefill_sm100_kernel<true, 2, true, false, false>,
+        prefill_sm100_kernel<false, 2, false, true, false>,  prefill_sm100_kernel<true, 2, false, true, false>,
+        prefill_sm100_kernel<true, 1, true, true, false>,    prefill_sm100_kernel<true, 2, true, true, false>,
+        prefill_sm100_kernel<false, 2, false, false, true>,  prefill_sm100_kernel<false, 1, true, false, true>,
+        prefill_sm100_kernel<false, 2, true, false, true>,   prefill_sm100_kernel<false, 2, false, true, true>,
+        prefill_sm100_kernel<false, 1, true, true, true>,    prefill_sm100_kernel<false, 2, true, true, true>};
     const int form = p.d < 128 ? 1 + boxes : (p.general || (p.remote_only && !p.causal)) ? 1 : 0;
-    const int which = form + (halves ? 4 : 0);
+    const int which = p.window > 0 ? 8 + (p.d < 128 ? boxes : 0) + (halves ? 3 : 0) : form + (halves ? 4 : 0);
     const uint32_t smem = smem_bytes(boxes);
-    static bool attr_set[64][8] = {};
+    static bool attr_set[64][14] = {};
     if (!attr_set[ctx->device & 63][which]) {
         cudaError_t e = cudaFuncSetAttribute(kernels[which], cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         // the register split inside the kernel has to fit into what the launch allocates: an increase that

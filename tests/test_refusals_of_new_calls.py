@@ -24,6 +24,10 @@ def call(name, **over):
                                       vsc=P, k=P, v=P, stream=None),
         "fedattn_decode_quant": dict(ctx=C.addressof(CTX), shape=C.byref(shape), mode=0, q=P, kc=P, ksc=P, vc=P, vsc=P, cap=32, len=P,
                                      max=32, window=0, sink=0, o=P, lse=None, stream=None),
+        "fedattn_local_window": dict(ctx=C.addressof(CTX), shape=C.byref(shape), q=P, k=P, v=P, cu=(C.c_int32 * 3)(0, 4, 9), window=4,
+                                     sink=1, o=P, lse=None, stream=None),
+        "fedattn_decode_window": dict(ctx=C.addressof(CTX), shape=C.byref(shape), mode=0, q=P, k=P, v=P, stride=2048, len=P, max=16,
+                                      window=4, sink=1, o=P, lse=None, stream=None),
     }[name]
     unknown = set(over) - set(args)
     assert not unknown, unknown
@@ -56,6 +60,14 @@ INVALID = [
     ("fedattn_decode_quant", o) for o in (
         dict(ctx=None), dict(shape=None), dict(mode=2), dict(q=None), dict(o=None), dict(len=None), dict(q=P + 2), dict(o=P + 8),
         dict(cap=24), dict(max=33), dict(max=-1), dict(kc=None), dict(vc=P + 4), dict(window=-1), dict(sink=-1), dict(sink=3))
+] + [
+    ("fedattn_local_window", o) for o in (
+        dict(ctx=None), dict(shape=None), dict(cu=None), dict(window=0), dict(window=-2), dict(sink=-1), dict(q=None), dict(k=None),
+        dict(o=None), dict(v=P + 8), dict(cu=(C.c_int32 * 3)(1, 4, 9)), dict(cu=(C.c_int32 * 3)(0, 4, 3)))
+] + [
+    ("fedattn_decode_window", o) for o in (
+        dict(ctx=None), dict(shape=None), dict(mode=2), dict(q=None), dict(k=None), dict(len=None), dict(o=P + 8), dict(max=-1),
+        dict(stride=-8), dict(stride=4), dict(window=0), dict(sink=-1))
 ]
 
 
@@ -75,6 +87,7 @@ def test_workspace_too_small():
 
 
 def test_nothing_to_do():
+    assert call("fedattn_local_window", cu=(C.c_int32 * 3)(0, 0, 0)) == 0
     assert call("fedattn_qk_norm_rope", n=0) == 0
     assert call("fedattn_qk_norm_rope", q=None, qo=None, k=None, ko=None) == 0
     assert call("fedattn_quantize_kv", n=0) == 0
