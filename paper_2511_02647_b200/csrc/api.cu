@@ -194,14 +194,15 @@ fedattn_status fedattn_create(fedattn_ctx **out, int device, void *workspace, si
     if (device < 0 || device >= count) return FEDATTN_ERR_CUDA;
     DeviceGuard g(device);
     if (g.err != cudaSuccess) return status_of(g.err);
-    cudaDeviceProp prop;
-    err = cudaGetDeviceProperties(&prop, device);
+    int sm_count = 0, major = 0;
+    err = cudaDeviceGetAttribute(&sm_count, cudaDevAttrMultiProcessorCount, device);
+    if (err == cudaSuccess) err = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device);
     if (err != cudaSuccess) return status_of(err);
     fedattn_ctx *ctx = new (std::nothrow) fedattn_ctx();
     if (!ctx) return FEDATTN_ERR_CUDA;
     Context &c = ctx->c;
     c.device = device;
-    c.sm_count = prop.multiProcessorCount;
+    c.sm_count = sm_count;
     c.workspace = static_cast<char *>(workspace);
     c.workspace_bytes = workspace_bytes;
     c.status = reinterpret_cast<int32_t *>(workspace);
@@ -212,7 +213,7 @@ fedattn_status fedattn_create(fedattn_ctx **out, int device, void *workspace, si
     c.agg_seq = 0;
     c.agg_key = ~0ull;
     c.encode_tiled = nullptr;
-    if (prop.major == 10) {
+    if (major == 10) {
         void *fn = nullptr;
         cudaDriverEntryPointQueryResult qres;
         if (status_of(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres)) == FEDATTN_OK &&
@@ -442,8 +443,8 @@ fedattn_status fedattn_qk_norm_rope(fedattn_ctx *ctx, const fedattn_shape *shape
     for (int i = 0; i < rot_dim / 2; ++i) {
         if (!(fabs(inv_freq_host[i]) <= 1e18)) return FEDATTN_ERR_INVALID_ARG;
         // turns per position; whole ones do not matter
-        long double turn = fmodl((long double)inv_freq_host[i] / 6.283185307179586476925286766559L, 1.0L);
-        if (turn < 0) turn += 1.0L;
+        long double turn = (long double)inv_freq_host[i] * 0.15915494309189533576888376337251436L;
+        if (!(turn >= 0.0L && turn < 1.0L)) turn -= floorl(turn);
         turn *= 18446744073709551616.0L;
         p.freq[i] = turn >= 18446744073709551615.5L ? 0 : (uint64_t)(turn + 0.5L);
     }
@@ -456,7 +457,7 @@ fedattn_status fedattn_qk_norm_rope(fedattn_ctx *ctx, const fedattn_shape *shape
     p.q = q; p.k = k; p.wq = q_weight; p.wk = k_weight; p.qo = q_out; p.ko = k_out;
     p.n_rows = n_rows; p.d = d; p.rot = rot_dim; p.interleaved = interleaved; p.eps = eps; p.pos = pos;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t err = launch_qk_norm_rope(p, shape->dtype, ctx->c.sm_count, s, &ctx->c.launches);
+    const cudaError_t err = launch_qk_norm_rope(p, shape->dtype, ctx->c.device, ctx->c.sm_count, s, &ctx->c.launches);
     if (err == cudaSuccess) front_note(ctx->c.device, s, false);
     return status_of(err);
 }
@@ -553,10 +554,7 @@ fedattn_status fedattn_decode_quant(fedattn_ctx *ctx, const fedattn_shape *shape
     p.sync = mode == FEDATTN_DECODE_SYNC; p.cap = cap_rows; p.kv_len = kv_len; p.max_kv_len = max_kv_len;
     p.window = window; p.n_sink = n_sink;
     p.partial = reinterpret_cast<float *>(ctx->c.scratch); p.partial_bytes = ctx->c.scratch_bytes;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const cudaError_t err = launch_decode_quant(p, shape->dtype, ctx->c.device, ctx->c.sm_count, s, &ctx->c.launches);
-    if (err == cudaSuccess) front_note(ctx->c.device, s, false);
-    return status_of(err);
+    return status_of(launch_decode_quant(p, shape->dtype, ctx->c.device, ctx->c.sm_count, static_cast<cudaStream_t>(stream), &ctx->c.launches));
 }
 
 }  // extern "C"

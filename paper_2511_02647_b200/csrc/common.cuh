@@ -267,7 +267,7 @@ struct RopeParams {
     const int32_t *pos;           // nullable (= row index)
     uint64_t freq[FEDATTN_MAX_HEAD_DIM / 2];     // turns per position, in units of 2^-64, modulo a turn
 };
-cudaError_t launch_qk_norm_rope(const RopeParams &p, int dtype, int sm_count, cudaStream_t s, int64_t *launches);
+cudaError_t launch_qk_norm_rope(const RopeParams &p, int dtype, int device, int sm_count, cudaStream_t s, int64_t *launches);
 
 // ---- the 4-bit cache ------------------------------------------------------------------------------------
 struct QuantRows {
@@ -295,6 +295,7 @@ struct QuantDecodeParams {
     int32_t max_kv_len, window, n_sink;          // window 0: every key
     float *partial;               // scratch
     size_t partial_bytes;
+    int32_t early;                // inputs may be read before the preceding grid is complete (set by the launcher)
 };
 size_t decode_quant_scratch_bytes(int n_part, int hq, int d);
 cudaError_t launch_decode_quant(const QuantDecodeParams &p, int dtype, int device, int sm_count, cudaStream_t s, int64_t *launches);

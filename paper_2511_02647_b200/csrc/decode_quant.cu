@@ -30,6 +30,7 @@ constexpr int kThreads = 32 * kWarps;
 constexpr int kTileKeys = 32;
 constexpr int kMaxSlots = 64;                                   // partials per output row in the workspace
 constexpr int kMaxCluster = 8;
+constexpr float kRescale = 8.f;                                 // log2 units
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
 {
@@ -89,8 +90,6 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v)
 {
     *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
-__device__ __forceinline__ float load1(const float *p) { return *p; }
-__device__ __forceinline__ float load1(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 
 // Which keys a cache of `len` rows shows: [0, a) and [b, len).  The walk goes over tiles of kTileKeys keys: 0 .. n_a - 1, then t_b ...
 struct Walk {
@@ -134,9 +133,9 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
     constexpr int kW = L::kW, kKs = 2 * kW, kParts = L::kParts, kRows = 8 * kNT, kMt = kD / 16, kStages = L::kStages;
     extern __shared__ __align__(16) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, t = lane & 3;
-    grid_wait();                                                // nothing is read or written before
-    // (the merge kernel of this call, the only grid that can follow, waits for this one's end before it reads)
-    if (!kOneLaunch) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // Inputs are read before the preceding grid of the stream is known to be complete unless they may be its outputs.
+    if (!p.early) grid_wait();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int split = blockIdx.x, kvh = blockIdx.y;
     const int cache = blockIdx.z / n_chunks, chunk = blockIdx.z - cache * n_chunks;
     const int g = p.hq / p.hkv;
@@ -157,25 +156,24 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
     uint8_t *ring = smem + L::kQBytes + warp * L::kRing;
     // Pieces of 16 bytes.  Rows are copied up to the length, rounded up to 16 rows (the cache has them); what lies behind that in a tile is
     // whatever was there: finite, and masked.  128 channels: the pieces of rows 2, 3, 6, 7, .. of V change places in pairs, which
-    // spreads the reads of rows t over the banks.
+    // spreads the reads of rows t over the banks (row i / 4 of piece i: its bit 1 flips bit 1 of the piece).
+    const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
+    const int v_shift = kD == 128 ? ((lane ^ ((lane >> 2) & 2)) - lane) * 16 : 0;
+    const uint8_t *k_lane = kc + lane * 16, *v_lane = vc + lane * 16, *s_lane = (lane < 16 ? ks : vs) + (lane & 15) * 16;
     auto load_tile = [&](int tile, int stage) {
-        const int key0 = walk.key0(tile), rows = min(kTileKeys, (walk.len - key0 + 15) & ~15);
-        const uint32_t dst = (uint32_t)__cvta_generic_to_shared(ring + stage * L::kStageBytes);
-        const uint8_t *k_src = kc + (int64_t)key0 * L::kCodeRow, *v_src = vc + (int64_t)key0 * L::kCodeRow;
-        constexpr int kPieces = L::kCodeBytes / 16, kRowPieces = L::kCodeRow / 16;
+        const int key0 = walk.key0(tile), rows = (walk.len - key0 + 15) & ~15;
+        const uint32_t dst = ring_s + stage * L::kStageBytes;
+        const uint8_t *k_src = k_lane + (int64_t)key0 * L::kCodeRow, *v_src = v_lane + (int64_t)key0 * L::kCodeRow;
+        constexpr int kPieces = L::kCodeBytes / 16, kRowPieces = L::kCodeRow / 16, kScalePieces = L::kScaleBytes / 16;
+        const bool whole = rows >= kTileKeys;
 #pragma unroll
-        for (int i0 = 0; i0 < kPieces; i0 += 32) {
-            const int i = i0 + lane;
-            const int j = kD == 128 ? i ^ ((i >> 2) & 2) : i;   // (row i / 4: bit 1 of it flips bit 1 of the piece)
-            if (i < rows * kRowPieces) {
-                cp_async16(dst + i * 16, k_src + i * 16);
-                cp_async16(dst + L::kCodeBytes + j * 16, v_src + i * 16);
+        for (int i0 = 0; i0 < kPieces; i0 += 32)
+            if (whole ? kPieces % 32 == 0 || i0 + lane < kPieces : i0 + lane < rows * kRowPieces) {
+                cp_async16(dst + i0 * 16, k_src + i0 * 16);
+                cp_async16(dst + L::kCodeBytes + i0 * 16 + v_shift, v_src + i0 * 16);
             }
-        }
-        const uint8_t *s_src = lane < 16 ? ks : vs;
-        const int i = lane & 15;
-        if (i < rows * L::kScaleRow / 16)
-            cp_async16(dst + 2 * L::kCodeBytes + (lane >> 4) * L::kScaleBytes + i * 16, s_src + (int64_t)key0 * L::kScaleRow + i * 16);
+        if ((lane & 15) < (whole ? kScalePieces : rows * L::kScaleRow / 16))
+            cp_async16(dst + 2 * L::kCodeBytes + (lane >> 4) * (L::kScaleBytes - 256), s_lane + (int64_t)key0 * L::kScaleRow);
     };
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) {
@@ -192,9 +190,7 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = 0.f;
         if (row < rows_here) {
-            const T *src = static_cast<const T *>(p.q) + out_row(chunk * kRows + row) * kD + 8 * x;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = load1(src + e);
+            load8(static_cast<const T *>(p.q) + out_row(chunk * kRows + row) * kD + 8 * x, v);
         }
         const int qt = x / kW, w = x - qt * kW;
 #pragma unroll
@@ -247,7 +243,9 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-            for (int n = 0; n < kNT; ++n) s[mt][n][0] = s[mt][n][1] = s[mt][n][2] = s[mt][n][3] = 0.f;
+            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[mt][n][c] = 0.f;
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
             uint32_t code[2][kW];
@@ -272,7 +270,7 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
                     const int grp = (t * kW + w) >> 2;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        sc[e] = scale_pair(sKs[(16 * mt + 8 * e + my_key) * L::kScaleRow + grp] * 0x10001u);
+                        sc[e] = scale_pair(sKs[(16 * mt + 8 * e + my_key) * L::kScaleRow + grp]);
                         of[e] = offset_pair(sc[e]);
                     }
                 }
@@ -297,24 +295,29 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
         // ---- mask, online softmax: a row's 32 keys are 4 values in each of the 8 lanes with the same t ----
         const int key0 = walk.key0(tile);
         const bool full = key0 + kTileKeys <= walk.a || (key0 >= walk.b && key0 + kTileKeys <= walk.len);
-        uint32_t pf[kParts][kNT][2][2];                         // P^T as operand B: [row tile of keys][half]
-#pragma unroll
-        for (int n = 0; n < kNT; ++n) {
-            float mx[2] = {-INFINITY, -INFINITY};
+        if (!full) {                                            // (-inf stays -inf under a positive factor)
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const bool see = full || walk.sees(key0 + 16 * mt + 8 * (c >> 1) + my_key);
-                    s[mt][n][c] = see ? s[mt][n][c] * sl2 : -INFINITY;
-                    mx[c & 1] = fmaxf(mx[c & 1], s[mt][n][c]);
-                }
+                for (int e = 0; e < 2; ++e)
+                    if (!walk.sees(key0 + 16 * mt + 8 * e + my_key))
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) {
-                mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
-                mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
-            }
-            if (__any_sync(0xffffffffu, mx[0] > m[n][0] || mx[1] > m[n][1])) {
+                        for (int n = 0; n < kNT; ++n) s[mt][n][2 * e] = s[mt][n][2 * e + 1] = -INFINITY;
+        }
+        uint32_t pf[kParts][kNT][2][2];                         // P^T as operand B: [row tile of keys][half]
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) {
+            // The reference of a row moves when one of its lanes has seen a logit more than 2^8 above it: one vote per tile, and the
+            // shuffles only then.
+            float mx[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) mx[e] = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e])) * sl2;
+            if (__any_sync(0xffffffffu, mx[0] > m[n][0] + kRescale || mx[1] > m[n][1] + kRescale)) {
+#pragma unroll
+                for (int o = 4; o < 32; o <<= 1) {
+                    mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
+                    mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const float mn = fmaxf(m[n][e], mx[e]), al = mn == -INFINITY ? 1.f : ex2(m[n][e] - mn);
@@ -329,7 +332,7 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    s[mt][n][c] = ex2(s[mt][n][c] - ref[c & 1]);
+                    s[mt][n][c] = ex2(fmaf(s[mt][n][c], sl2, -ref[c & 1]));
                     l[n][c & 1] += s[mt][n][c];
                 }
 #pragma unroll
@@ -371,7 +374,7 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const uint8_t *src = sVs + (16 * mt + 8 * e + t) * L::kScaleRow + grp;
-                        sc[e] = scale_pair(src[0] | (uint32_t)src[4 * L::kScaleRow] << 16);
+                        sc[e] = scale_pair(src[0], src[4 * L::kScaleRow]);
                         of[e] = offset_pair(sc[e]);
                     }
                 }
@@ -416,6 +419,8 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
                 *reinterpret_cast<float4 *>(dst + 2 * i) = make_float4(acc[n][i][e], acc[n][i][2 + e], acc[n][i + 1][e], acc[n][i + 1][2 + e]);
         }
     __syncthreads();
+    // The workspace may still be read by the merge of the previous call; outputs and this grid's end come behind the wait too.
+    if (!kOneLaunch) grid_wait();
     // ---- fold the warps: a warp per row, four channels per lane; into the first warp's row, or the workspace ----
     for (int row = warp; row < rows_here; row += kWarps) {
         float *src = part + row * L::kPartialRow;
@@ -448,6 +453,7 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     if (n_splits > 1) cluster.sync(); else __syncthreads();
+    grid_wait();                                                // before the first write
     for (int row = split + n_splits * warp; row < rows_here; row += n_splits * kWarps) {
         float2 ml[kMaxCluster];
         float4 v[kMaxCluster];
@@ -481,66 +487,71 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
     if (n_splits > 1) cluster.sync();                           // peers may still be reading this CTA's partials
 }
 
-// A CTA per output row: four groups of slots by 32 lanes of four channels.
+// A CTA takes output rows blockIdx.x, blockIdx.x + gridDim.x, ...: four groups of slots by 32 lanes of four channels.  At most one CTA
+// per SM, and small: the next call's stream kernel is launched when every CTA of this grid has started.
 constexpr int kMergeGroups = 4;
 template <typename T>
 __global__ void __launch_bounds__(32 * kMergeGroups)
-decode_quant_merge_kernel(const float *partial, T *out, float *lse, int d, int n_slots)
+decode_quant_merge_kernel(const float *partial, T *out, float *lse, int d, int n_slots, int n_rows)
 {
     __shared__ float4 s_o[kMergeGroups][32];
     __shared__ float2 s_ml[kMergeGroups];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     grid_wait();                                                // the partials of this call
     const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
-    const int64_t orow = blockIdx.x;
-    const float *src = partial + orow * n_slots * (d + 4);
     const bool mine = 4 * lane < d;
-    float mm = -INFINITY, ll = 0.f;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = grp; k0 < n_slots; k0 += 4 * kMergeGroups) {
-        float2 ml[4];
-        float4 v[4];
-        float mn = mm;
+    for (int64_t orow = blockIdx.x; orow < n_rows; orow += gridDim.x) {
+        const float *src = partial + orow * n_slots * (d + 4);
+        float mm = -INFINITY, ll = 0.f;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k0 = grp; k0 < n_slots; k0 += 4 * kMergeGroups) {
+            float2 ml[4];
+            float4 v[4];
+            float mn = mm;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int slot = k0 + k * kMergeGroups;
-            ml[k] = make_float2(-INFINITY, 0.f);
-            v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (slot < n_slots) {
-                ml[k] = ld_partial2(src + slot * (d + 4));
-                if (mine) v[k] = ld_partial4(src + slot * (d + 4) + 4 + 4 * lane);
+            for (int k = 0; k < 4; ++k) {
+                const int slot = k0 + k * kMergeGroups;
+                ml[k] = make_float2(-INFINITY, 0.f);
+                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (slot < n_slots) {
+                    ml[k] = ld_partial2(src + slot * (d + 4));
+                    if (mine) v[k] = ld_partial4(src + slot * (d + 4) + 4 + 4 * lane);
+                }
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mn = fmaxf(mn, ml[k].x);
+            const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(mm - ref);
+            ll *= f0; a.x *= f0; a.y *= f0; a.z *= f0; a.w *= f0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = ex2(ml[k].x - ref);             // 0 for an empty partial
+                ll += ml[k].y * f;
+                a.x += v[k].x * f; a.y += v[k].y * f; a.z += v[k].z * f; a.w += v[k].w * f;
+            }
+            mm = mn;
         }
+        s_o[grp][lane] = a;
+        if (lane == 0) s_ml[grp] = make_float2(mm, ll);
+        __syncthreads();
+        if (grp == 0) {
+            float mx = -INFINITY, z = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mn = fmaxf(mn, ml[k].x);
-        const float ref = mn == -INFINITY ? 0.f : mn, f0 = ex2(mm - ref);
-        ll *= f0; a.x *= f0; a.y *= f0; a.z *= f0; a.w *= f0;
+            for (int q = 0; q < kMergeGroups; ++q) mx = fmaxf(mx, s_ml[q].x);
+            const float ref = mx == -INFINITY ? 0.f : mx;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float f = ex2(ml[k].x - ref);                 // 0 for an empty partial
-            ll += ml[k].y * f;
-            a.x += v[k].x * f; a.y += v[k].y * f; a.z += v[k].z * f; a.w += v[k].w * f;
+            for (int q = 0; q < kMergeGroups; ++q) {
+                const float f = ex2(s_ml[q].x - ref);
+                const float4 v = s_o[q][lane];
+                z += s_ml[q].y * f;
+                o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+            }
+            const float inv = z > 0.f ? 1.f / z : 0.f;
+            if (mine) store4(out + orow * d + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+            if (lane == 0 && lse) lse[orow] = z > 0.f ? lse_exact(mx, z) : -INFINITY;
         }
-        mm = mn;
+        __syncthreads();                                        // the group buffers are reused by the next row
     }
-    s_o[grp][lane] = a;
-    if (lane == 0) s_ml[grp] = make_float2(mm, ll);
-    __syncthreads();
-    if (grp != 0) return;
-    float mx = -INFINITY, z = 0.f;
-#pragma unroll
-    for (int q = 0; q < kMergeGroups; ++q) mx = fmaxf(mx, s_ml[q].x);
-    const float ref = mx == -INFINITY ? 0.f : mx;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int q = 0; q < kMergeGroups; ++q) {
-        const float f = ex2(s_ml[q].x - ref);
-        const float4 v = s_o[q][lane];
-        z += s_ml[q].y * f;
-        o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
-    }
-    const float inv = z > 0.f ? 1.f / z : 0.f;
-    if (mine) store4(out + orow * d + 4 * lane, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (lane == 0 && lse) lse[orow] = z > 0.f ? lse_exact(mx, z) : -INFINITY;
 }
 
 typedef void (*Kernel)(const QuantDecodeParams, int, int);
@@ -571,8 +582,9 @@ size_t decode_quant_scratch_bytes(int n_part, int hq, int d)
     return d % kQuantGroup == 0 ? (size_t)n_part * hq * kMaxSlots * (d + 4) * sizeof(float) : 0;
 }
 
-cudaError_t launch_decode_quant(const QuantDecodeParams &p, int dtype, int device, int sm_count, cudaStream_t s, int64_t *launches)
+cudaError_t launch_decode_quant(const QuantDecodeParams &p_in, int dtype, int device, int sm_count, cudaStream_t s, int64_t *launches)
 {
+    QuantDecodeParams p = p_in;
     const int g = p.hq / p.hkv, rows_total = p.sync ? p.n_part * g : g, caches = p.sync ? 1 : p.n_part;
     const bool f32 = dtype == FEDATTN_F32;
     const int nt = rows_total <= 8 ? 1 : (rows_total <= 16 || f32 ? 2 : 4);
@@ -589,8 +601,6 @@ cudaError_t launch_decode_quant(const QuantDecodeParams &p, int dtype, int devic
     if (n_splits > kMaxSlots) n_splits = kMaxSlots;
     if (n_splits < 1) n_splits = 1;
     bool one_launch = n_splits <= kMaxCluster;
-    if (one_launch)
-        while (n_splits & (n_splits - 1)) n_splits &= n_splits - 1;
     if (!one_launch && (size_t)p.n_part * p.hq * n_splits * (p.d + 4) * sizeof(float) > p.partial_bytes) return cudaErrorInvalidValue;
     typedef __nv_bfloat16 bf;
     const Variant v = one_launch ? (f32 ? variant_of<float, true>(p.d, nt) : variant_of<bf, true>(p.d, nt))
@@ -602,21 +612,42 @@ cudaError_t launch_decode_quant(const QuantDecodeParams &p, int dtype, int devic
         if (e != cudaSuccess) return e;
         set = true;
     }
-    WaitFirstLaunch l(dim3((unsigned)n_splits, (unsigned)p.hkv, (unsigned)(caches * n_chunks)), dim3(kThreads), v.smem, s);
-    if (one_launch) {
-        l.attr[1].id = cudaLaunchAttributeClusterDimension;
-        l.attr[1].val.clusterDim.x = (unsigned)n_splits; l.attr[1].val.clusterDim.y = 1; l.attr[1].val.clusterDim.z = 1;
-        l.cfg.numAttrs = 2;
-    }
-    cudaError_t e = cudaLaunchKernelEx(&l.cfg, v.kernel, p, (int)n_splits, n_chunks);
+    // may the stream kernel read its inputs before the preceding grid of the stream is complete?
+    const size_t rows = (size_t)caches * p.hkv * p.cap, code_bytes = rows * (p.d / 2), scale_bytes = rows * (p.d / kQuantGroup);
+    const size_t qo_bytes = (size_t)p.n_part * p.hq * p.d * (f32 ? 4 : 2);
+    const MemRange in[6] = {{p.q, qo_bytes}, {p.k_codes, code_bytes}, {p.k_scales, scale_bytes}, {p.v_codes, code_bytes},
+                            {p.v_scales, scale_bytes}, {p.kv_len, caches * sizeof(int32_t)}};
+    const MemRange out[2] = {{p.o, qo_bytes}, {p.lse, p.lse ? (size_t)p.n_part * p.hq * sizeof(float) : 0}};
+    // (The record costs a short call 0.5 us of the host, 4.5 -> 5.0 us in a loop of 4 x 700 keys of 64 channels; replayed from a graph
+    // the early start takes it from 4.2 to 1.5.)
+    const EarlyStart es = early_start(device, s, in, 6, out, 2);
+    p.early = es.early ? 1 : 0;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)n_splits; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3((unsigned)n_splits, (unsigned)p.hkv, (unsigned)(caches * n_chunks));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = v.smem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = one_launch ? 2 : 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, v.kernel, p, (int)n_splits, n_chunks);
     ++*launches;
-    if (e != cudaSuccess || one_launch) return e != cudaSuccess ? e : cudaGetLastError();
-    WaitFirstLaunch ml(dim3((unsigned)(p.n_part * p.hq)), dim3(32 * kMergeGroups), 0, s);
+    if (e != cudaSuccess || one_launch) return early_start_end(es, e != cudaSuccess ? e : cudaGetLastError());
+    const int n_rows = p.n_part * p.hq, per_cta = (n_rows + sm_count - 1) / sm_count;
+    cfg.gridDim = dim3((unsigned)((n_rows + per_cta - 1) / per_cta));
+    cfg.blockDim = dim3(32 * kMergeGroups);
+    cfg.dynamicSmemBytes = 0;
+    cfg.numAttrs = 1;
     const float *partial = p.partial;
-    e = f32 ? cudaLaunchKernelEx(&ml.cfg, decode_quant_merge_kernel<float>, partial, static_cast<float *>(p.o), p.lse, (int)p.d, (int)n_splits)
-            : cudaLaunchKernelEx(&ml.cfg, decode_quant_merge_kernel<bf>, partial, static_cast<bf *>(p.o), p.lse, (int)p.d, (int)n_splits);
+    e = f32 ? cudaLaunchKernelEx(&cfg, decode_quant_merge_kernel<float>, partial, static_cast<float *>(p.o), p.lse, (int)p.d, (int)n_splits, n_rows)
+            : cudaLaunchKernelEx(&cfg, decode_quant_merge_kernel<bf>, partial, static_cast<bf *>(p.o), p.lse, (int)p.d, (int)n_splits, n_rows);
     ++*launches;
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return early_start_end(es, e != cudaSuccess ? e : cudaGetLastError());
 }
 
 }  // namespace fedattn

@@ -2,10 +2,15 @@
 // on one side, the storage type on the other.
 //
 // Scale of a group: the least of the 256 whose sevenfold reaches the group's largest magnitude.  Code: x / scale to the nearest
-// integer, ties to the even one, -7 .. 7.  Both are exact decisions: 7 * scale and code * scale are exact in fp32 (7 and 8
-// significant bits), so comparisons with them carry no rounding, and what an approximate quotient gets wrong is put right.
+// integer, ties to the even one, -7 .. 7.  Both are exact decisions, although the quotients are not.  scale = m * 2^e with 8 <= m <= 15.
+//   bf16: x is at most 255 times a power of two, so x / scale lies on a tie or at least 1 / 960 away from it (twice the quotient is a
+//   fraction over m * 2^5 at the most where it is near an odd number), and amax / 7 on a scale or 2^-9 of itself away.  Rounding the
+//   product with 1 / scale to a multiple of 2^-13 first puts it on the tie when it belongs there.
+//   fp32: comparisons put right what the approximate quotient gets wrong: 7 * scale and code * scale are exact in fp32 (7 and 8
+//   significant bits), and so is x minus the latter near a tie.
 //
-// A warp takes one row of one of the two tensors; a lane 8 channels at a time, four lanes a group.
+// A warp takes the same head of neighbouring rows at a time (2 of 128 channels), so that what it writes to the cache is one run of 128
+// bytes when the rows are neighbours there; a lane has 8 channels, four lanes a group.
 #include "quant_cache.cuh"
 
 namespace fedattn {
@@ -13,45 +18,52 @@ namespace fedattn {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kBatch = 4;                                       // heads of a warp, whose loads are in flight together
 
 // the least scale byte with 7 * scale >= amax (255 when none has)
-__device__ __forceinline__ uint32_t scale_byte(float amax)
+template <typename T> __device__ __forceinline__ uint32_t scale_byte(float amax)
 {
-    // 1/7 rounded: the guess is off by one step at most, and the comparisons decide
-    const int bits = __float_as_int(amax * 0.14285715f);
-    int b = (bits >> 20) - ((127 - 18) << 3);                   // exponent and three mantissa bits, rounded down
+    // 1/7 rounded down, so that a product that should be a scale does not pass it; then up to four significant bits
+    const int bits = __float_as_int(amax * __int_as_float(0x3e124924));
+    int b = ((bits + 0xfffff) >> 20) - ((127 - 18) << 3);
     b = max(0, min(255, b));
-    if (7.f * scale_float(b) < amax && b < 255) ++b;
-    if (7.f * scale_float(b) < amax && b < 255) ++b;
-    if (b > 0 && 7.f * scale_float(b - 1) >= amax) --b;
+    if (sizeof(T) == 4 && 7.f * scale_float(b) < amax && b < 255) ++b;
     return (uint32_t)b;
 }
 
-// x / scale, to nearest, ties to even, within -7 .. 7; offset by 8
-__device__ __forceinline__ uint32_t code_of(float x, float scale, float inv)
+// eight codes, offset by 8, as nibbles
+template <typename T> __device__ __forceinline__ uint32_t codes_of(float (&x)[8], float scale, bool saturated);
+template <> __device__ __forceinline__ uint32_t codes_of<__nv_bfloat16>(float (&x)[8], float scale, bool saturated)
 {
-    const float ax = fabsf(x);
-    float n = rintf(fminf(ax * inv, 8.f));
-    const float rest = fmaf(-n, scale, ax), half = 0.5f * scale;
-    const bool odd = ((int)n & 1) != 0;
-    if (rest > half || (rest == half && odd)) n += 1.f;
-    else if (rest < -half || (rest == -half && odd)) n -= 1.f;
-    n = fminf(n, 7.f);
-    return (uint32_t)(8 + (int)copysignf(n, x));
-}
-
-template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8]);
-template <> __device__ __forceinline__ void load8<float>(const float *p, float (&x)[8])
-{
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16 *p, float (&x)[8])
-{
-    const uint4 v = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if (saturated)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        for (int e = 0; e < 8; ++e) x[e] = fminf(fmaxf(x[e], -7.f * scale), 7.f * scale);
+    const float inv = 1.f / scale;
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 7; e >= 0; --e) {
+        // to a multiple of 2^-13, then to an integer in the low bits of the sum
+        const float t = __fadd_rn(__fadd_rn(__fmul_rn(x[e], inv), 1536.f), -1536.f);
+        w = w * 16 + (__float_as_uint(__fadd_rn(t, 12582920.f)) & 15u);
+    }
+    return w;
+}
+template <> __device__ __forceinline__ uint32_t codes_of<float>(float (&x)[8], float scale, bool)
+{
+    const float inv = 1.f / scale, half = 0.5f * scale;
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 7; e >= 0; --e) {
+        const float ax = fabsf(x[e]);
+        float n = rintf(fminf(ax * inv, 8.f));
+        const float rest = fmaf(-n, scale, ax);
+        const bool odd = ((int)n & 1) != 0;
+        if (rest > half || (rest == half && odd)) n += 1.f;
+        else if (rest < -half || (rest == -half && odd)) n -= 1.f;
+        n = fminf(n, 7.f);
+        w = w * 16 + (uint32_t)(8 + (int)copysignf(n, x[e]));
+    }
+    return w;
 }
 
 // the row of the cache that row i stands for, or -1 where there is none (skipped, or out of range: status)
@@ -59,49 +71,62 @@ __device__ __forceinline__ int64_t cache_row(const QuantRows &p, int64_t i)
 {
     const int64_t at = p.at ? (int64_t)ld_int(p.at + i) : i;
     if (at >= p.n_caches * p.cap) {
-        if ((threadIdx.x & 31) == 0) atomicMax(p.status, (int32_t)FEDATTN_ERR_INDEX);
+        atomicMax(p.status, (int32_t)FEDATTN_ERR_INDEX);
         return -1;
     }
     return at;
 }
 
+// What a lane works on: a row, and 8 channels of each of kBatch heads of K or V.
+template <int kD> struct LaneWork {
+    static constexpr int kVecs = kD / 8, kRows = 32 / kVecs;    // lanes of a head, rows of a warp
+    int64_t row;
+    int c, head0, vec;
+    bool is_v, mine;
+    __device__ LaneWork(const QuantRows &p, int n_chunks)
+    {
+        const int lane = threadIdx.x & 31, r = lane / kVecs;
+        const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+        const int64_t rest = unit / n_chunks;
+        vec = lane - r * kVecs;
+        c = vec * 8;
+        head0 = (int)(unit - rest * n_chunks) * kBatch;
+        is_v = rest & 1;
+        row = (rest >> 1) * kRows + r;
+        mine = r < kRows && row < p.n_rows;
+    }
+};
+
 template <typename T, int kD>
 __global__ void __launch_bounds__(kThreads)
-quantize_kernel(const __grid_constant__ QuantRows p)
+quantize_kernel(const __grid_constant__ QuantRows p, int n_chunks)
 {
-    constexpr int kVecs = kD / 8;                               // lanes of a head
-    const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     grid_wait();                                                // nothing is read or written before
-    if (unit >= 2 * p.n_rows) return;
-    const int64_t row = unit >> 1;
-    const bool is_v = unit & 1;
-    const int64_t at = cache_row(p, row);
-    if (at < 0) return;
-    const int64_t cache = at / p.cap, within = at - cache * p.cap;
-    const T *src = static_cast<const T *>(is_v ? p.v : p.k) + row * (is_v ? p.v_stride : p.k_stride);
-    uint8_t *codes = is_v ? p.v_codes : p.k_codes, *scales = is_v ? p.v_scales : p.k_scales;
-    const int n = p.hkv * kVecs;
-#pragma unroll 4
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const int i = i0 + lane, h = i / kVecs, c = (i - h * kVecs) * 8;
-        float x[8], amax = 0.f;
+    const LaneWork<kD> w(p, n_chunks);
+    const int64_t at = w.mine ? cache_row(p, w.row) : -1;
+    const int64_t cache = at >= 0 ? at / p.cap : 0, within = at - cache * p.cap;
+    const T *src = static_cast<const T *>(w.is_v ? p.v : p.k) + w.row * (w.is_v ? p.v_stride : p.k_stride) + w.c;
+    uint8_t *codes = w.is_v ? p.v_codes : p.k_codes, *scales = w.is_v ? p.v_scales : p.k_scales;
+    float x[kBatch][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        if (i < n) load8(src + (int64_t)h * kD + c, x);
+    for (int u = 0; u < kBatch; ++u) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
+        for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
+        if (at >= 0 && w.head0 + u < p.hkv) load8(src + (int64_t)(w.head0 + u) * kD, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+        float amax = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[u][e]));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-        const uint32_t b = scale_byte(amax);
-        const float scale = scale_float(b), inv = 1.f / scale;
-        uint32_t w = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w |= code_of(x[e], scale, inv) << (4 * e);
-        if (i < n) {
-            const int64_t r = (cache * p.hkv + h) * p.cap + within;
-            *reinterpret_cast<uint32_t *>(codes + r * (kD / 2) + c / 2) = w;
-            if ((i & 3) == 0) scales[r * (kD / kQuantGroup) + c / kQuantGroup] = (uint8_t)b;
+        const uint32_t b = scale_byte<T>(amax);
+        const uint32_t word = codes_of<T>(x[u], scale_float(b), b == 255);
+        if (at >= 0 && w.head0 + u < p.hkv) {
+            const int64_t r = (cache * p.hkv + w.head0 + u) * p.cap + within;
+            *reinterpret_cast<uint32_t *>(codes + r * (kD / 2) + w.c / 2) = word;
+            if ((w.vec & 3) == 0) scales[r * (kD / kQuantGroup) + w.c / kQuantGroup] = (uint8_t)b;
         }
     }
 }
@@ -123,34 +148,36 @@ template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 
 
 template <typename T, int kD>
 __global__ void __launch_bounds__(kThreads)
-dequantize_kernel(const __grid_constant__ QuantRows p)
+dequantize_kernel(const __grid_constant__ QuantRows p, int n_chunks)
 {
-    constexpr int kVecs = kD / 8;
-    const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     grid_wait();                                                // nothing is read or written before
-    if (unit >= 2 * p.n_rows) return;
-    const int64_t row = unit >> 1;
-    const bool is_v = unit & 1;
-    const int64_t at = cache_row(p, row);
+    const LaneWork<kD> w(p, n_chunks);
+    const int64_t at = w.mine ? cache_row(p, w.row) : -1;
     if (at < 0) return;
     const int64_t cache = at / p.cap, within = at - cache * p.cap;
-    T *dst = static_cast<T *>(is_v ? p.v_out : p.k_out) + row * p.hkv * kD;
-    const uint8_t *codes = is_v ? p.v_codes : p.k_codes, *scales = is_v ? p.v_scales : p.k_scales;
-    const int n = p.hkv * kVecs;
-#pragma unroll 4
-    for (int i = lane; i < n; i += 32) {
-        const int h = i / kVecs, c = (i - h * kVecs) * 8;
-        const int64_t r = (cache * p.hkv + h) * p.cap + within;
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(codes + r * (kD / 2) + c / 2);
-        const uint32_t s = scale_pair(scales[r * (kD / kQuantGroup) + c / kQuantGroup] * 0x10001u), off = offset_pair(s);
-        const uint32_t pair[4] = {nibble_pair<0>(w, s, off), nibble_pair<1>(w, s, off), nibble_pair<2>(w, s, off), nibble_pair<3>(w, s, off)};
-        store8(dst + (int64_t)h * kD + c, pair);
+    T *dst = static_cast<T *>(w.is_v ? p.v_out : p.k_out) + w.row * p.hkv * kD + w.c;
+    const uint8_t *codes = w.is_v ? p.v_codes : p.k_codes, *scales = w.is_v ? p.v_scales : p.k_scales;
+    uint32_t word[kBatch], byte[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+        word[u] = byte[u] = 0;
+        if (w.head0 + u < p.hkv) {
+            const int64_t r = (cache * p.hkv + w.head0 + u) * p.cap + within;
+            word[u] = *reinterpret_cast<const uint32_t *>(codes + r * (kD / 2) + w.c / 2);
+            byte[u] = scales[r * (kD / kQuantGroup) + w.c / kQuantGroup];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+        const uint32_t s = scale_pair(byte[u]), off = offset_pair(s);
+        const uint32_t pair[4] = {nibble_pair<0>(word[u], s, off), nibble_pair<1>(word[u], s, off), nibble_pair<2>(word[u], s, off),
+                                  nibble_pair<3>(word[u], s, off)};
+        if (w.head0 + u < p.hkv) store8(dst + (int64_t)(w.head0 + u) * kD, pair);
     }
 }
 
 template <typename T>
-void (*rows_kernel(int d, bool back))(const QuantRows)
+void (*rows_kernel(int d, bool back))(const QuantRows, int)
 {
     switch (d) {
     case 32: return back ? dequantize_kernel<T, 32> : quantize_kernel<T, 32>;
@@ -164,10 +191,11 @@ void (*rows_kernel(int d, bool back))(const QuantRows)
 
 cudaError_t launch_quant_rows(const QuantRows &p, bool back, int dtype, int d, cudaStream_t s, int64_t *launches)
 {
-    const int64_t blocks = (2 * p.n_rows + kThreads / 32 - 1) / (kThreads / 32);
+    const int n_chunks = (p.hkv + kBatch - 1) / kBatch, rows = 32 / (d / 8);
+    const int64_t units = 2 * ((p.n_rows + rows - 1) / rows) * n_chunks, blocks = (units + kThreads / 32 - 1) / (kThreads / 32);
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
     WaitFirstLaunch l(dim3((unsigned)blocks), dim3(kThreads), 0, s);
-    const cudaError_t e = cudaLaunchKernelEx(&l.cfg, dtype == FEDATTN_BF16 ? rows_kernel<__nv_bfloat16>(d, back) : rows_kernel<float>(d, back), p);
+    const cudaError_t e = cudaLaunchKernelEx(&l.cfg, dtype == FEDATTN_BF16 ? rows_kernel<__nv_bfloat16>(d, back) : rows_kernel<float>(d, back), p, n_chunks);
     ++*launches;
     return e != cudaSuccess ? e : cudaGetLastError();
 }

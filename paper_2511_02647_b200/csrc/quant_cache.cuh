@@ -12,8 +12,10 @@ namespace fedattn {
 
 constexpr int kQuantGroup = 32;
 
-// scale bytes in the low byte of either half -> a bf16 pair: the byte is the exponent's lower bits and three of the mantissa
-__device__ __forceinline__ uint32_t scale_pair(uint32_t bytes) { return (bytes << 4) + 0x36803680u; }
+// two scale bytes -> a bf16 pair: a byte is the exponent's lower bits and three of the mantissa.  (Multiplications and additions: the
+// pipe for shifts and selections is the one that the conversion fills.)
+__device__ __forceinline__ uint32_t scale_pair(uint32_t lo, uint32_t hi) { return hi * 0x00100000u + (lo * 0x10u + 0x36803680u); }
+__device__ __forceinline__ uint32_t scale_pair(uint32_t both) { return both * 0x00100010u + 0x36803680u; }
 __device__ __forceinline__ float scale_float(uint32_t byte) { return __uint_as_float(((byte << 4) + 0x3680u) << 16); }
 
 __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c)
@@ -33,7 +35,26 @@ __device__ __forceinline__ uint32_t offset_pair(uint32_t scale)
 // The nibbles at bits 4 kAt .. of either half of x as bf16 values: 128 + nibble is 0x4300 | nibble.
 template <int kAt> __device__ __forceinline__ uint32_t nibble_pair(uint32_t x, uint32_t scale, uint32_t offset)
 {
-    return fma_bf16x2(((x >> (4 * kAt)) & 0x000f000fu) | 0x43004300u, scale, offset);
+    // (one selection: written as two operations it was compiled to two.  Shifts as upper halves of products, which other units take:
+    // slower, one of three 10.2 -> 11.1 us, all three 12.5, decode of 8 x 4096 rows.)
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(x >> (4 * kAt)), "r"(0x000f000fu), "r"(0x43004300u));      // (a & b) | c
+    return fma_bf16x2(y, scale, offset);
+}
+
+// eight channels as fp32
+template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8]);
+template <> __device__ __forceinline__ void load8<float>(const float *p, float (&x)[8])
+{
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16 *p, float (&x)[8])
+{
+    const uint4 v = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
 }
 
 }  // namespace fedattn

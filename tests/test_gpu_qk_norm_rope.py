@@ -63,6 +63,35 @@ def test_rows_of_a_joint_projection_without_weights_and_positions(dtype):
     assert torch.equal(xd, before)
 
 
+@pytest.mark.parametrize("dtype,d,rot,inter,hq,hkv,rows", [("bf16", 128, 128, False, 4, 1, 5003), ("bf16", 64, 64, True, 3, 1, 9001),
+                                                           ("bf16", 72, 40, False, 2, 2, 5001), ("f32", 96, 48, False, 4, 2, 4999),
+                                                           ("f32", 64, 0, False, 2, 1, 9003), ("bf16", 128, 16, True, 32, 8, 2411),
+                                                           ("bf16", 128, 128, False, 96, 16, 1300)])
+def test_many_rows(dtype, d, rot, inter, hq, hkv, rows):
+    """Enough rows for every warp to walk several of them; one head of zeros, rows of a joint projection, then in place."""
+    rng = np.random.default_rng([d, rows])
+    x = ref.rounded(rng.standard_normal((rows, (hq + hkv) * d + 8)), dtype)
+    x[:, :d] = 0
+    wq, wk = (ref.rounded(1 + 0.3 * rng.standard_normal(d), dtype) for _ in range(2))
+    pos = rng.integers(0, 1 << 20, rows)
+    xd = dev(x.astype(np.float32), dtype)
+    shape = fa.Shape(1, hq, hkv, d, fa.BF16 if dtype == "bf16" else fa.F32)
+    ctx = fa.Context(shape, rows, rows)
+    q, k = xd[:, :hq * d].unflatten(1, (hq, d)), xd[:, hq * d:(hq + hkv) * d].unflatten(1, (hkv, d))
+    qo, ko = torch.full((rows, hq, d), float("nan"), dtype=xd.dtype, device="cuda"), torch.full((rows, hkv, d), float("nan"), dtype=xd.dtype, device="cuda")
+    rest = (dev(wq.astype(np.float32), dtype), dev(wk.astype(np.float32), dtype), 1e-6, torch.tensor(pos, dtype=torch.int32, device="cuda"), freqs(rot), inter)
+    fa.fedattn_qk_norm_rope(ctx, shape, q, k, *rest, qo, ko)
+    for got, a, h, w in ((qo, 0, hq, wq), (ko, hq * d, hkv, wk)):
+        want, size = ref.norm_rope(x[:, a:a + h * d].reshape(rows, h, d), w, float(np.float32(1e-6)), pos, freqs(rot), inter)
+        close(host(got), want, size, dtype)
+    q, k = q.contiguous(), k.contiguous()
+    fa.fedattn_qk_norm_rope(ctx, shape, q, k, *rest, q, k)
+    assert torch.equal(q, qo) and torch.equal(k, ko)
+    k.copy_(xd[:, hq * d:(hq + hkv) * d].unflatten(1, (hkv, d)))
+    fa.fedattn_qk_norm_rope(ctx, shape, None, k, *rest, None, k)
+    assert torch.equal(k, ko)
+
+
 def test_in_place_alone_and_on_another_stream():
     rows, hq, hkv, d = 257, 4, 4, 64
     rng = np.random.default_rng(6)
