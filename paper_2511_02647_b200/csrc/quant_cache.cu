@@ -66,10 +66,10 @@ template <> __device__ __forceinline__ uint32_t codes_of<float>(float (&x)[8], f
     return w;
 }
 
-// the row of the cache that row i stands for, or -1 where there is none (skipped, or out of range: status)
-__device__ __forceinline__ int64_t cache_row(const QuantRows &p, int64_t i)
+// the row of the caches that row i stands for, or -1 where there is none (skipped, or out of range: status).  (There are fewer than 2^31.)
+__device__ __forceinline__ int cache_row(const QuantRows &p, int i)
 {
-    const int64_t at = p.at ? (int64_t)ld_int(p.at + i) : i;
+    const int at = p.at ? ld_int(p.at + i) : i;
     if (at >= p.n_caches * p.cap) {
         atomicMax(p.status, (int32_t)FEDATTN_ERR_INDEX);
         return -1;
@@ -77,43 +77,49 @@ __device__ __forceinline__ int64_t cache_row(const QuantRows &p, int64_t i)
     return at;
 }
 
-// What a lane works on: a row, and 8 channels of each of kBatch heads of K or V.
+// What a lane works on: a row, and 8 channels of each of kBatch heads of K (even blockIdx.y) or V.
 template <int kD> struct LaneWork {
     static constexpr int kVecs = kD / 8, kRows = 32 / kVecs;    // lanes of a head, rows of a warp
-    int64_t row;
-    int c, head0, vec;
+    int row, c, head0, vec;
     bool is_v, mine;
-    __device__ LaneWork(const QuantRows &p, int n_chunks)
+    __device__ explicit LaneWork(const QuantRows &p)
     {
         const int lane = threadIdx.x & 31, r = lane / kVecs;
-        const int64_t unit = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-        const int64_t rest = unit / n_chunks;
+        const int64_t first = ((int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5)) * kRows;
         vec = lane - r * kVecs;
         c = vec * 8;
-        head0 = (int)(unit - rest * n_chunks) * kBatch;
-        is_v = rest & 1;
-        row = (rest >> 1) * kRows + r;
-        mine = r < kRows && row < p.n_rows;
+        head0 = (int)(blockIdx.y >> 1) * kBatch;
+        is_v = blockIdx.y & 1;
+        mine = r < kRows && first + r < p.n_rows;
+        row = mine ? (int)first + r : 0;
+    }
+    // flat row of head0 in the codes and scales
+    __device__ int64_t place(const QuantRows &p, int at) const
+    {
+        const int cap = (int)p.cap, cache = at / cap;
+        return ((int64_t)cache * p.hkv + head0) * cap + (at - cache * cap);
     }
 };
 
 template <typename T, int kD>
 __global__ void __launch_bounds__(kThreads)
-quantize_kernel(const __grid_constant__ QuantRows p, int n_chunks)
+quantize_kernel(const __grid_constant__ QuantRows p)
 {
     grid_wait();                                                // nothing is read or written before
-    const LaneWork<kD> w(p, n_chunks);
-    const int64_t at = w.mine ? cache_row(p, w.row) : -1;
-    const int64_t cache = at >= 0 ? at / p.cap : 0, within = at - cache * p.cap;
-    const T *src = static_cast<const T *>(w.is_v ? p.v : p.k) + w.row * (w.is_v ? p.v_stride : p.k_stride) + w.c;
+    const LaneWork<kD> w(p);
+    const int at = w.mine ? cache_row(p, w.row) : -1;
+    const T *src = static_cast<const T *>(w.is_v ? p.v : p.k) + w.row * (w.is_v ? p.v_stride : p.k_stride) + (int64_t)w.head0 * kD + w.c;
     uint8_t *codes = w.is_v ? p.v_codes : p.k_codes, *scales = w.is_v ? p.v_scales : p.k_scales;
     float x[kBatch][8];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
-        if (at >= 0 && w.head0 + u < p.hkv) load8(src + (int64_t)(w.head0 + u) * kD, x[u]);
+        if (w.mine && w.head0 + u < p.hkv) load8(src + u * kD, x[u]);
     }
+    const int64_t r0 = at >= 0 ? w.place(p, at) : 0;
+    codes += r0 * (kD / 2) + w.c / 2;
+    scales += r0 * (kD / kQuantGroup) + w.c / kQuantGroup;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
         float amax = 0.f;
@@ -124,9 +130,8 @@ quantize_kernel(const __grid_constant__ QuantRows p, int n_chunks)
         const uint32_t b = scale_byte<T>(amax);
         const uint32_t word = codes_of<T>(x[u], scale_float(b), b == 255);
         if (at >= 0 && w.head0 + u < p.hkv) {
-            const int64_t r = (cache * p.hkv + w.head0 + u) * p.cap + within;
-            *reinterpret_cast<uint32_t *>(codes + r * (kD / 2) + w.c / 2) = word;
-            if ((w.vec & 3) == 0) scales[r * (kD / kQuantGroup) + w.c / kQuantGroup] = (uint8_t)b;
+            *reinterpret_cast<uint32_t *>(codes + u * p.cap * (kD / 2)) = word;
+            if ((w.vec & 3) == 0) scales[u * p.cap * (kD / kQuantGroup)] = (uint8_t)b;
         }
     }
 }
@@ -148,23 +153,23 @@ template <> __device__ __forceinline__ void store8<__nv_bfloat16>(__nv_bfloat16 
 
 template <typename T, int kD>
 __global__ void __launch_bounds__(kThreads)
-dequantize_kernel(const __grid_constant__ QuantRows p, int n_chunks)
+dequantize_kernel(const __grid_constant__ QuantRows p)
 {
     grid_wait();                                                // nothing is read or written before
-    const LaneWork<kD> w(p, n_chunks);
-    const int64_t at = w.mine ? cache_row(p, w.row) : -1;
+    const LaneWork<kD> w(p);
+    const int at = w.mine ? cache_row(p, w.row) : -1;
     if (at < 0) return;
-    const int64_t cache = at / p.cap, within = at - cache * p.cap;
-    T *dst = static_cast<T *>(w.is_v ? p.v_out : p.k_out) + w.row * p.hkv * kD + w.c;
-    const uint8_t *codes = w.is_v ? p.v_codes : p.k_codes, *scales = w.is_v ? p.v_scales : p.k_scales;
+    T *dst = static_cast<T *>(w.is_v ? p.v_out : p.k_out) + ((int64_t)w.row * p.hkv + w.head0) * kD + w.c;
+    const int64_t r0 = w.place(p, at);
+    const uint8_t *codes = (w.is_v ? p.v_codes : p.k_codes) + r0 * (kD / 2) + w.c / 2;
+    const uint8_t *scales = (w.is_v ? p.v_scales : p.k_scales) + r0 * (kD / kQuantGroup) + w.c / kQuantGroup;
     uint32_t word[kBatch], byte[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
         word[u] = byte[u] = 0;
         if (w.head0 + u < p.hkv) {
-            const int64_t r = (cache * p.hkv + w.head0 + u) * p.cap + within;
-            word[u] = *reinterpret_cast<const uint32_t *>(codes + r * (kD / 2) + w.c / 2);
-            byte[u] = scales[r * (kD / kQuantGroup) + w.c / kQuantGroup];
+            word[u] = *reinterpret_cast<const uint32_t *>(codes + u * p.cap * (kD / 2));
+            byte[u] = scales[u * p.cap * (kD / kQuantGroup)];
         }
     }
 #pragma unroll
@@ -172,12 +177,12 @@ dequantize_kernel(const __grid_constant__ QuantRows p, int n_chunks)
         const uint32_t s = scale_pair(byte[u]), off = offset_pair(s);
         const uint32_t pair[4] = {nibble_pair<0>(word[u], s, off), nibble_pair<1>(word[u], s, off), nibble_pair<2>(word[u], s, off),
                                   nibble_pair<3>(word[u], s, off)};
-        if (w.head0 + u < p.hkv) store8(dst + (int64_t)(w.head0 + u) * kD, pair);
+        if (w.head0 + u < p.hkv) store8(dst + u * kD, pair);
     }
 }
 
 template <typename T>
-void (*rows_kernel(int d, bool back))(const QuantRows, int)
+void (*rows_kernel(int d, bool back))(const QuantRows)
 {
     switch (d) {
     case 32: return back ? dequantize_kernel<T, 32> : quantize_kernel<T, 32>;
@@ -191,11 +196,11 @@ void (*rows_kernel(int d, bool back))(const QuantRows, int)
 
 cudaError_t launch_quant_rows(const QuantRows &p, bool back, int dtype, int d, cudaStream_t s, int64_t *launches)
 {
-    const int n_chunks = (p.hkv + kBatch - 1) / kBatch, rows = 32 / (d / 8);
-    const int64_t units = 2 * ((p.n_rows + rows - 1) / rows) * n_chunks, blocks = (units + kThreads / 32 - 1) / (kThreads / 32);
-    if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
-    WaitFirstLaunch l(dim3((unsigned)blocks), dim3(kThreads), 0, s);
-    const cudaError_t e = cudaLaunchKernelEx(&l.cfg, dtype == FEDATTN_BF16 ? rows_kernel<__nv_bfloat16>(d, back) : rows_kernel<float>(d, back), p, n_chunks);
+    const int rows = 32 / (d / 8) * (kThreads / 32);            // of a CTA
+    const int64_t blocks = (p.n_rows + rows - 1) / rows, pieces = 2 * (((int64_t)p.hkv + kBatch - 1) / kBatch);
+    if (pieces > 65535) return cudaErrorInvalidValue;           // grid
+    WaitFirstLaunch l(dim3((unsigned)blocks, (unsigned)pieces), dim3(kThreads), 0, s);
+    const cudaError_t e = cudaLaunchKernelEx(&l.cfg, dtype == FEDATTN_BF16 ? rows_kernel<__nv_bfloat16>(d, back) : rows_kernel<float>(d, back), p);
     ++*launches;
     return e != cudaSuccess ? e : cudaGetLastError();
 }
