@@ -474,7 +474,9 @@ cudaError_t launch_instance(const GenericParams &p, TiledPlan plan, int sm_count
     // (kKeyWarps = 1: 93 and 280 us with one pair against 107 and 341 with two, local and sync of 2048 rows x 16 heads).
     const int64_t key_tiles = (max_kv + L::kKeys - 1) / L::kKeys, units = (int64_t)plan.n_tiles * p.hkv;
     plan.splits = 1;
-    while (plan.splits < kMaxCluster && units * plan.splits <= sm_count && plan.splits * 2 <= key_tiles) plan.splits *= 2;
+    // (Through a window the walks are short and latency is all: two CTAs per SM.  Bidirectional window of 100, 845 rows of 8 heads of 64 channels
+    // 40.1 -> 29.4 us, 600 rows of 8 heads of 128 44.2 -> 39.0; three and four per SM 33.7 and 52.0.)
+    while (plan.splits < kMaxCluster && units * plan.splits <= (kWindow ? 2 : 1) * sm_count && plan.splits * 2 <= key_tiles) plan.splits *= 2;
     const int64_t per_cta = (key_tiles + plan.splits - 1) / plan.splits;     // tiles of a CTA, at most
     plan.stages = 1;
     while (kKeyWarps > 1 && plan.stages < kMaxStages && plan.stages < per_cta && L::bytes(plan.stages + 1) <= kMost) ++plan.stages;

@@ -125,8 +125,11 @@ template <typename T, int kD, int kNT> struct Layout {
     static constexpr bool kQInRegs = kNT * kParts <= 2;
 };
 
+// Registers: with two (three) CTAs per SM a CTA of the merge kernel still finds its 6144.  It has to: the next call's stream kernel is
+// launched when all of those have started.  (243 registers, what 32 rows take without the limit: 8 participants over 32 768 rows 27.1 us, with
+// 224 and 60 bytes spilled 19.9, 208 21.0.)
 template <typename T, int kD, int kNT, bool kOneLaunch>
-__global__ void __launch_bounds__(kThreads, kNT == 4 || sizeof(T) == 4 ? 2 : 3)
+__global__ void __maxnreg__((kNT == 4 || sizeof(T) == 4 ? 224 : 152))
 decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, int n_chunks)
 {
     using L = Layout<T, kD, kNT>;
