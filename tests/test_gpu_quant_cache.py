@@ -151,6 +151,38 @@ def test_long_shared_caches_take_the_two_launch_form(dtype, n, hq, hkv, d, lengt
     assert ctx.launch_count() - before == 2
 
 
+@pytest.mark.parametrize("mode,n,hq,hkv,lens,window,sink,spread", [
+    ("sync", 8, 8, 2, [9001], 0, 0, 1.0), ("sync", 8, 8, 2, [2049], 0, 0, 40.0), ("sync", 5, 8, 2, [2300], 0, 0, 0.0),
+    ("sync", 17, 8, 2, [3333], 0, 0, 1.0), ("sync", 8, 16, 4, [20000], 5000, 4, 1.0), ("sync", 8, 8, 2, [2500], 2200, 300, 8.0),
+    ("sync", 8, 8, 2, [2560], 1, 2040, 1.0), ("local", 3, 24, 1, [0, 2100, 129], 0, 0, 1.0), ("local", 2, 64, 2, [5000, 127], 0, 0, 3.0),
+    ("sync", 8, 8, 2, [1], 0, 0, 1.0), ("sync", 8, 8, 2, [0], 0, 0, 1.0)])
+def test_many_rows_to_a_key(mode, n, hq, hkv, lens, window, sink, spread):
+    """More than 16 query rows share the keys of long caches: four column tiles to a warp, several chunks of rows."""
+    cap = max(-(-max(lens) // 16) * 16, 4096)
+    decode(fa.DECODE_SYNC if mode == "sync" else fa.DECODE_LOCAL, "bf16", n, hq, hkv, 128, lens, cap, window, sink, spread, most=max(max(lens), 4096))
+
+
+def test_references_that_grow_along_the_walk():
+    """Keys whose logits rise from tile to tile by far more than 2^8 a time, and fall again."""
+    d, n, hq, length = 128, 8, 4, 4096
+    shape = fa.Shape(n, hq, 1, d, fa.BF16)
+    ctx = fa.Context(shape, n, length)
+    rng = np.random.default_rng(8)
+    level = np.concatenate([np.linspace(-60, 60, length // 2), np.linspace(60, -60, length // 2)])
+    k = rng.standard_normal((1, 1, length, d)) * 0.1 + (level / d ** 0.5)[None, None, :, None]
+    v = rng.standard_normal((1, 1, length, d))
+    (kc, kb), (vc, vb) = ref.quantise(ref.rounded(k, "bf16")), ref.quantise(ref.rounded(v, "bf16"))
+    cache = fa.QuantCache(shape, 1, length, *(torch.from_numpy(x).cuda() for x in
+                          (ref.pack(kc), kb.astype(np.uint8), ref.pack(vc), vb.astype(np.uint8))))
+    q = ref.rounded(np.abs(rng.standard_normal((n, hq, d))) + 0.5, "bf16")
+    o, lse = torch.empty((n, hq, d), dtype=torch.bfloat16, device="cuda"), torch.empty((n, hq), device="cuda")
+    fa.fedattn_decode_quant(ctx, shape, fa.DECODE_SYNC, dev(q.astype(np.float32), "bf16"), cache,
+                            torch.tensor([length], dtype=torch.int32, device="cuda"), length, o, lse)
+    assert ctx.poll() == 0
+    want = ref.attend(q, ref.values(kc, kb)[0].transpose(1, 0, 2), ref.values(vc, vb)[0].transpose(1, 0, 2), np.ones((n, length), bool), d ** -0.5)
+    ref.check_attention(host(o), host(lse), want, "bf16")
+
+
 @pytest.mark.parametrize("spread", [0.0, 30.0, 3000.0])
 def test_flat_and_steep_rows(spread):
     decode(fa.DECODE_LOCAL, "bf16", 3, 8, 2, 128, [300, 47, 160], 304, spread=spread)
