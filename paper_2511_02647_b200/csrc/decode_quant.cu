@@ -12,7 +12,7 @@
 //     words side by side (one byte permutation for eight elements) make the pairs that run along the keys.
 //   * A warp has tiles of 32 keys of its own and its own ring of asynchronous copies: no barrier between warps during the walk.  Head-major
 //     rows make every copy a run of consecutive bytes.
-// The exponent reference follows every new maximum, so the heaviest key weighs 1, which bf16 holds.  fp32 queries go in as three bf16
+// The exponent reference of a row moves when its maximum has grown by more than 2^8 (one vote per tile).  fp32 queries go in as three bf16
 // parts, and so do their weights (24 bits): six products for two.
 //
 // Up to 8 splits of a (cache, KV head) are one cluster and one launch; more are merged by a second kernel out of the workspace.
@@ -133,7 +133,7 @@ __global__ void __maxnreg__((kNT == 4 || sizeof(T) == 4 ? 224 : 152))
 decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, int n_chunks)
 {
     using L = Layout<T, kD, kNT>;
-    constexpr int kW = L::kW, kKs = 2 * kW, kParts = L::kParts, kRows = 8 * kNT, kMt = kD / 16, kStages = L::kStages;
+    constexpr int kW = L::kW, kParts = L::kParts, kRows = 8 * kNT, kMt = kD / 16, kStages = L::kStages;
     extern __shared__ __align__(16) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, t = lane & 3;
     // Inputs are read before the preceding grid of the stream is known to be complete unless they may be its outputs.
@@ -149,6 +149,15 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
         return (int64_t)part * p.hq + kvh * g + sub;
     };
 
+    // the rows of Q on their way while the length is: word x of row i / (kD / 8), i = tid + kThreads j
+    constexpr int kQWords = kRows * (kD / 8), kQEach = (kQWords + kThreads - 1) / kThreads;
+    Eight<T> raw[kQEach];
+#pragma unroll
+    for (int j = 0; j < kQEach; ++j) {
+        const int i = tid + kThreads * j, row = i / (kD / 8);
+        raw[j].zero();
+        if (i < kQWords && row < rows_here) raw[j].load(static_cast<const T *>(p.q) + out_row(chunk * kRows + row) * kD + 8 * (i - row * (kD / 8)));
+    }
     const Walk walk(p, cache);
     const int per = (walk.n_tiles + n_splits - 1) / n_splits;
     const int tile_lo = min(split * per, walk.n_tiles), tile_hi = min(tile_lo + per, walk.n_tiles);
@@ -186,33 +195,29 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
 
     // ---- Q as operand B: [part][column tile][step][lane] pairs of pairs ----
     // Step 2 w + h of a lane: word w of its quarter of the channels, nibble pairs 2 h and 2 h + 1 (nibbles i and i + 4).
-    uint2 *sq = reinterpret_cast<uint2 *>(smem);
-    for (int i = tid; i < kRows * (kD / 8); i += kThreads) {
-        const int row = i / (kD / 8), x = i - row * (kD / 8);   // word x of the row's channels
-        float v[8];
+    // (Both steps of a word lie side by side.)
+    uint4 *sq = reinterpret_cast<uint4 *>(smem);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.f;
-        if (row < rows_here) {
-            load8(static_cast<const T *>(p.q) + out_row(chunk * kRows + row) * kD + 8 * x, v);
-        }
-        const int qt = x / kW, w = x - qt * kW;
+    for (int j = 0; j < kQEach; ++j) {
+        const int i = tid + kThreads * j, row = i / (kD / 8), x = i - row * (kD / 8), qt = x / kW, w = x - qt * kW;
+        if (i >= kQWords) break;
+        float v[8];
+        raw[j].get(v);
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
             uint32_t pr[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) pr[e] = take_part(v[e], v[e + 4]);
-            uint2 *dst = sq + ((part * kNT + (row >> 3)) * kKs + 2 * w) * 32 + (row & 7) * 4 + qt;
-            dst[0] = make_uint2(pr[0], pr[1]);
-            dst[32] = make_uint2(pr[2], pr[3]);
+            sq[((part * kNT + (row >> 3)) * kW + w) * 32 + (row & 7) * 4 + qt] = make_uint4(pr[0], pr[1], pr[2], pr[3]);
         }
     }
     __syncthreads();
-    uint2 qf[L::kQInRegs ? kNT * kParts : 1][kKs];
+    uint4 qf[L::kQInRegs ? kNT * kParts : 1][kW];
     if (L::kQInRegs) {
 #pragma unroll
         for (int n = 0; n < kNT * kParts; ++n)
 #pragma unroll
-            for (int s = 0; s < kKs; ++s) qf[n][s] = sq[(n * kKs + s) * 32 + lane];
+            for (int w = 0; w < kW; ++w) qf[n][w] = sq[(n * kW + w) * 32 + lane];
     }
 
     const float sl2 = p.scale * 1.4426950408889634f;
@@ -249,50 +254,53 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
             for (int n = 0; n < kNT; ++n)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) s[mt][n][c] = 0.f;
+        uint32_t code[2][2][kW];                                // keys 16 mt + 8 e + my_key
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
-            uint32_t code[2][kW];
+        for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const uint8_t *src = sK + (16 * mt + 8 * e + my_key) * L::kCodeRow + t * (kD / 8);
                 if (kW == 4) {
                     const uint4 x = *reinterpret_cast<const uint4 *>(src);
-                    code[e][0] = x.x; code[e][1] = x.y; code[e][2 % kW] = x.z; code[e][3 % kW] = x.w;
+                    code[mt][e][0] = x.x; code[mt][e][1] = x.y; code[mt][e][2 % kW] = x.z; code[mt][e][3 % kW] = x.w;
                 } else if (kW == 2) {
                     const uint2 x = *reinterpret_cast<const uint2 *>(src);
-                    code[e][0] = x.x; code[e][1 % kW] = x.y;
+                    code[mt][e][0] = x.x; code[mt][e][1 % kW] = x.y;
                 } else {
 #pragma unroll
-                    for (int w = 0; w < kW; ++w) code[e][w] = reinterpret_cast<const uint32_t *>(src)[w];
+                    for (int w = 0; w < kW; ++w) code[mt][e][w] = reinterpret_cast<const uint32_t *>(src)[w];
                 }
             }
-            uint32_t sc[2], of[2];
+        uint32_t sc[2][2], of[2][2];
 #pragma unroll
-            for (int w = 0; w < kW; ++w) {
-                if (w == 0 || kW == 3) {                        // the group of this word; 96 channels: a quarter may touch two
-                    const int grp = (t * kW + w) >> 2;
+        for (int w = 0; w < kW; ++w) {
+            uint32_t a[2][2][4];                                // [half of the word][row tile]
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        sc[e] = scale_pair(sKs[(16 * mt + 8 * e + my_key) * L::kScaleRow + grp]);
-                        of[e] = offset_pair(sc[e]);
+            for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (w == 0 || kW == 3) {                    // the group of this word; 96 channels: a quarter may touch two
+                        sc[mt][e] = scale_pair(sKs[(16 * mt + 8 * e + my_key) * L::kScaleRow + ((t * kW + w) >> 2)]);
+                        of[mt][e] = offset_pair(sc[mt][e]);
                     }
+                    const uint32_t x = code[mt][e][w];
+                    a[0][mt][e] = nibble_pair<0>(x, sc[mt][e], of[mt][e]);
+                    a[0][mt][2 + e] = nibble_pair<1>(x, sc[mt][e], of[mt][e]);
+                    a[1][mt][e] = nibble_pair<2>(x, sc[mt][e], of[mt][e]);
+                    a[1][mt][2 + e] = nibble_pair<3>(x, sc[mt][e], of[mt][e]);
                 }
+            // products on one sum stand as far apart as they can
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t a[4];
+            for (int part = 0; part < kParts; ++part) {
+                uint4 b[kNT];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        a[e] = h ? nibble_pair<2>(code[e][w], sc[e], of[e]) : nibble_pair<0>(code[e][w], sc[e], of[e]);
-                        a[2 + e] = h ? nibble_pair<3>(code[e][w], sc[e], of[e]) : nibble_pair<1>(code[e][w], sc[e], of[e]);
-                    }
+                for (int n = 0; n < kNT; ++n) b[n] = L::kQInRegs ? qf[part * kNT + n][w] : sq[((part * kNT + n) * kW + w) * 32 + lane];
 #pragma unroll
-                    for (int part = 0; part < kParts; ++part)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int n = 0; n < kNT; ++n) {
-                            const uint2 b = L::kQInRegs ? qf[part * kNT + n][2 * w + h] : sq[((part * kNT + n) * kKs + 2 * w + h) * 32 + lane];
-                            mma_bf16(s[mt][n], a, b.x, b.y);
-                        }
-                }
+                    for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt) mma_bf16(s[mt][n], a[h][mt], h ? b[n].z : b[n].x, h ? b[n].w : b[n].y);
             }
         }
         // ---- mask, online softmax: a row's 32 keys are 4 values in each of the 8 lanes with the same t ----
@@ -307,29 +315,33 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
 #pragma unroll
                         for (int n = 0; n < kNT; ++n) s[mt][n][2 * e] = s[mt][n][2 * e + 1] = -INFINITY;
         }
-        uint32_t pf[kParts][kNT][2][2];                         // P^T as operand B: [row tile of keys][half]
+        // The reference of a row moves when one of its lanes has seen a logit more than 2^8 above it: one vote per tile for all rows,
+        // and the shuffles only then.
+        float mx[kNT][2];
+        bool above = false;
 #pragma unroll
-        for (int n = 0; n < kNT; ++n) {
-            // The reference of a row moves when one of its lanes has seen a logit more than 2^8 above it: one vote per tile, and the
-            // shuffles only then.
-            float mx[2];
+        for (int n = 0; n < kNT; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) mx[e] = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e])) * sl2;
-            if (__any_sync(0xffffffffu, mx[0] > m[n][0] + kRescale || mx[1] > m[n][1] + kRescale)) {
+            for (int e = 0; e < 2; ++e) {
+                mx[n][e] = fmaxf(fmaxf(s[0][n][e], s[0][n][2 + e]), fmaxf(s[1][n][e], s[1][n][2 + e])) * sl2;
+                above = above || mx[n][e] > m[n][e] + kRescale;
+            }
+        if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
-                for (int o = 4; o < 32; o <<= 1) {
-                    mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], o));
-                    mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], o));
-                }
+            for (int n = 0; n < kNT; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float mn = fmaxf(m[n][e], mx[e]), al = mn == -INFINITY ? 1.f : ex2(m[n][e] - mn);
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xffffffffu, mx[n][e], o));
+                    const float mn = fmaxf(m[n][e], mx[n][e]), al = mn == -INFINITY ? 1.f : ex2(m[n][e] - mn);
                     m[n][e] = mn;
                     l[n][e] *= al;
 #pragma unroll
                     for (int i = 0; i < kMt; ++i) { acc[n][i][e] *= al; acc[n][i][2 + e] *= al; }
                 }
-            }
+        }
+#pragma unroll
+        for (int n = 0; n < kNT; ++n) {
             const float ref[2] = {m[n][0] == -INFINITY ? 0.f : m[n][0], m[n][1] == -INFINITY ? 0.f : m[n][1]};
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
@@ -338,15 +350,18 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
                     s[mt][n][c] = ex2(fmaf(s[mt][n][c], sl2, -ref[c & 1]));
                     l[n][c & 1] += s[mt][n][c];
                 }
+        }
+        uint32_t pf[kParts][kNT][2][2];                         // P^T as operand B: [row tile of keys][half]
 #pragma unroll
-            for (int part = 0; part < kParts; ++part)
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+            for (int n = 0; n < kNT; ++n)
 #pragma unroll
                 for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
                         pf[part][n][mt][e] = transpose8(kParts > 1 ? take_part(s[mt][n][2 * e], s[mt][n][2 * e + 1])
                                                                    : pack_bf16(s[mt][n][2 * e], s[mt][n][2 * e + 1]));
-        }
         // ---- O^T += V^T P^T ----
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
@@ -425,31 +440,39 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
     // The workspace may still be read by the merge of the previous call; outputs and this grid's end come behind the wait too.
     if (!kOneLaunch) grid_wait();
     // ---- fold the warps: a warp per row, four channels per lane; into the first warp's row, or the workspace ----
-    for (int row = warp; row < rows_here; row += kWarps) {
-        float *src = part + row * L::kPartialRow;
-        float2 ml[kWarps];
-        float mx = -INFINITY;
+    constexpr int kEach = kRows / kWarps, kFold = kEach < 4 ? kEach : 4;     // rows of a warp, and how many at a time
+#pragma unroll 1
+    for (int r0 = 0; r0 < kEach; r0 += kFold) {
+        float2 ml[kFold][kWarps];
+        float4 v[kFold][kWarps];
 #pragma unroll
-        for (int q = 0; q < kWarps; ++q) {
-            ml[q] = *reinterpret_cast<const float2 *>(src + q * kRows * L::kPartialRow);
-            mx = fmaxf(mx, ml[q].x);
-        }
-        const float ref = mx == -INFINITY ? 0.f : mx;
-        float z = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < kFold; ++i) {
+            const float *src = part + (warp + kWarps * (r0 + i)) * L::kPartialRow;
 #pragma unroll
-        for (int q = 0; q < kWarps; ++q) {
-            const float f = ex2(ml[q].x - ref);
-            z += ml[q].y * f;
-            if (4 * lane < kD) {
-                const float4 v = *reinterpret_cast<const float4 *>(src + q * kRows * L::kPartialRow + 4 + 4 * lane);
-                o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
+            for (int q = 0; q < kWarps; ++q) {
+                ml[i][q] = *reinterpret_cast<const float2 *>(src + q * kRows * L::kPartialRow);
+                v[i][q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (4 * lane < kD) v[i][q] = *reinterpret_cast<const float4 *>(src + q * kRows * L::kPartialRow + 4 + 4 * lane);
             }
         }
         __syncwarp();                                           // every lane has read the maxima and sums
-        float *dst = kOneLaunch ? src : p.partial + (out_row(chunk * kRows + row) * n_splits + split) * L::kPartialRow;
-        if (lane == 0) *reinterpret_cast<float2 *>(dst) = make_float2(mx, z);
-        if (4 * lane < kD) *reinterpret_cast<float4 *>(dst + 4 + 4 * lane) = o;
+#pragma unroll
+        for (int i = 0; i < kFold; ++i) {
+            const int row = warp + kWarps * (r0 + i);
+            const float mx = fmaxf(fmaxf(ml[i][0].x, ml[i][1].x), fmaxf(ml[i][2].x, ml[i][3].x)), ref = mx == -INFINITY ? 0.f : mx;
+            float z = 0.f;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int q = 0; q < kWarps; ++q) {
+                const float f = ex2(ml[i][q].x - ref);
+                z += ml[i][q].y * f;
+                o.x += v[i][q].x * f; o.y += v[i][q].y * f; o.z += v[i][q].z * f; o.w += v[i][q].w * f;
+            }
+            if (row >= rows_here) break;
+            float *dst = kOneLaunch ? part + row * L::kPartialRow : p.partial + (out_row(chunk * kRows + row) * n_splits + split) * L::kPartialRow;
+            if (lane == 0) *reinterpret_cast<float2 *>(dst) = make_float2(mx, z);
+            if (4 * lane < kD) *reinterpret_cast<float4 *>(dst + 4 + 4 * lane) = o;
+        }
     }
     if (!kOneLaunch) return;
     // ---- fold the CTAs of the cluster: rank q finishes rows q, q + n_splits, ... ----

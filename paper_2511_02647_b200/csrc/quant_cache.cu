@@ -110,25 +110,25 @@ quantize_kernel(const __grid_constant__ QuantRows p)
     const int at = w.mine ? cache_row(p, w.row) : -1;
     const T *src = static_cast<const T *>(w.is_v ? p.v : p.k) + w.row * (w.is_v ? p.v_stride : p.k_stride) + (int64_t)w.head0 * kD + w.c;
     uint8_t *codes = w.is_v ? p.v_codes : p.k_codes, *scales = w.is_v ? p.v_scales : p.k_scales;
-    float x[kBatch][8];
+    Eight<T> raw[kBatch];
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
-        if (w.mine && w.head0 + u < p.hkv) load8(src + u * kD, x[u]);
+        raw[u].zero();
+        if (w.mine && w.head0 + u < p.hkv) raw[u].load(src + u * kD);
     }
     const int64_t r0 = at >= 0 ? w.place(p, at) : 0;
     codes += r0 * (kD / 2) + w.c / 2;
     scales += r0 * (kD / kQuantGroup) + w.c / kQuantGroup;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-        float amax = 0.f;
+        float x[8], amax = 0.f;
+        raw[u].get(x);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[u][e]));
+        for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[e]));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
         const uint32_t b = scale_byte<T>(amax);
-        const uint32_t word = codes_of<T>(x[u], scale_float(b), b == 255);
+        const uint32_t word = codes_of<T>(x, scale_float(b), b == 255);
         if (at >= 0 && w.head0 + u < p.hkv) {
             *reinterpret_cast<uint32_t *>(codes + u * p.cap * (kD / 2)) = word;
             if ((w.vec & 3) == 0) scales[u * p.cap * (kD / kQuantGroup)] = (uint8_t)b;

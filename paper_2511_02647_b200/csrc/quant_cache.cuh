@@ -42,19 +42,27 @@ template <int kAt> __device__ __forceinline__ uint32_t nibble_pair(uint32_t x, u
     return fma_bf16x2(y, scale, offset);
 }
 
-// eight channels as fp32
-template <typename T> __device__ __forceinline__ void load8(const T *p, float (&x)[8]);
-template <> __device__ __forceinline__ void load8<float>(const float *p, float (&x)[8])
-{
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-template <> __device__ __forceinline__ void load8<__nv_bfloat16>(const __nv_bfloat16 *p, float (&x)[8])
-{
-    const uint4 v = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// eight channels: as they lie in memory, then as fp32
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    float4 a, b;
+    __device__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ void load(const float *p) { a = reinterpret_cast<const float4 *>(p)[0]; b = reinterpret_cast<const float4 *>(p)[1]; }
+    __device__ void get(float (&x)[8]) const
+    {
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    }
+};
+template <> struct Eight<__nv_bfloat16> {
+    uint4 v;
+    __device__ void zero() { v = make_uint4(0, 0, 0, 0); }
+    __device__ void load(const __nv_bfloat16 *p) { v = *reinterpret_cast<const uint4 *>(p); }
+    __device__ void get(float (&x)[8]) const
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
+        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+    }
+};
 
 }  // namespace fedattn
