@@ -263,17 +263,20 @@ qk_norm_rope_kernel(const __grid_constant__ RopeParams p, int per, int n_chunks,
 }
 
 // Many rows: a warp walks rows and keeps the next ones on their way into a ring of its own in shared memory (asynchronous copies), so
-// that what is in flight does not depend on registers: 16 warps of an SM held 32 KB in registers, 8 hold 80 KB here.
+// that what is in flight does not depend on registers: 16 warps of an SM held 32 KB in registers, 8 hold 80 KB here.  A CTA is one warp: as
+// many as the rings leave room for.  (13 633 rows of 32 + 8 heads of 128 channels, 279 MB, 42.7 us at the copy rate: loads to registers 58.7 us;
+// rings in CTAs of four warps 51.7, of two 50.8, of one 49.3 = 5.66 TB/s, with three stages 56.8.)
+constexpr int kRingThreads = 32;
 constexpr int kRingStages = 2;
 template <typename T, int kUnit, int kLanes, bool kInterleaved>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kRingThreads)
 qk_norm_rope_ring_kernel(const __grid_constant__ RopeParams p, int stage_bytes)
 {
     typedef Lane<T, kUnit, kLanes, kInterleaved> L;
     typedef typename L::U U;
     extern __shared__ __align__(16) uint8_t smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = p.d;
-    const int64_t first = (int64_t)blockIdx.x * (kThreads / 32) + warp, step = (int64_t)gridDim.x * (kThreads / 32);
+    const int64_t first = (int64_t)blockIdx.x * (kRingThreads / 32) + warp, step = (int64_t)gridDim.x * (kRingThreads / 32);
     uint8_t *ring = smem + (size_t)warp * kRingStages * stage_bytes;
     const uint32_t ring_s = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
     const int q_bytes = p.hq * d * (int)sizeof(T);
@@ -346,7 +349,7 @@ template <typename T, int kUnit, int kLanes> Form form_of(bool interleaved)
                        : Form{qk_norm_rope_kernel<T, kUnit, kLanes, false>, qk_norm_rope_ring_kernel<T, kUnit, kLanes, false>, 32 / kLanes};
 }
 
-constexpr int kRingMost = 24 * 1024;                            // bytes of a row in the ring: two CTAs of an SM hold 16 of them
+constexpr int kRingMost = 24 * 1024;                            // bytes of a row in a ring: an SM holds the rings of four warps
 
 }  // namespace
 
@@ -359,18 +362,18 @@ cudaError_t launch_qk_norm_rope(const RopeParams &p, int dtype, int device, int 
     const Form f = forms[which](il);
     const int n_heads = p.hq + p.hkv;
     const int64_t row_bytes = (int64_t)n_heads * p.d * (dtype == FEDATTN_BF16 ? 2 : 4);
-    // Rows that give every warp of two (or more) CTAs per SM a few go through the rings.
-    const int64_t ring_bytes = row_bytes * kRingStages * (kThreads / 32);
-    const int ctas = ring_bytes > 0 ? (int)(220 * 1024 / ring_bytes < 4 ? 220 * 1024 / ring_bytes : 4) : 0;
-    if (row_bytes <= kRingMost && ctas >= 1 && p.n_rows >= (int64_t)sm_count * ctas * (kThreads / 32) * 2) {
+    // The rings, when every warp that they leave room for gets two rows.
+    const int64_t ring_bytes = row_bytes * kRingStages * (kRingThreads / 32);
+    const int most = 16 * 32 / kRingThreads, fit = ring_bytes > 0 ? (int)(225 * 1024 / (ring_bytes + 1024)) : 0, ctas = fit < most ? fit : most;
+    if (row_bytes <= kRingMost && ctas >= 1 && p.n_rows >= (int64_t)sm_count * ctas * (kRingThreads / 32) * 2) {
         static bool attr_set[64][6][2] = {};
         bool &set = attr_set[device & 63][which][il];
         if (!set) {
-            const cudaError_t e = cudaFuncSetAttribute(f.many, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingMost * kRingStages * (kThreads / 32));
+            const cudaError_t e = cudaFuncSetAttribute(f.many, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingMost * kRingStages * (kRingThreads / 32));
             if (e != cudaSuccess) return e;
             set = true;
         }
-        WaitFirstLaunch l(dim3((unsigned)(sm_count * ctas)), dim3(kThreads), (size_t)ring_bytes, s);
+        WaitFirstLaunch l(dim3((unsigned)(sm_count * ctas)), dim3(kRingThreads), (size_t)ring_bytes, s);
         const cudaError_t e = cudaLaunchKernelEx(&l.cfg, f.many, p, (int)row_bytes);
         ++*launches;
         return e != cudaSuccess ? e : cudaGetLastError();

@@ -18,7 +18,9 @@ namespace fedattn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBatch = 4;                                       // heads of a warp, whose loads are in flight together
+// Heads of a warp, whose loads are in flight together.  (8192 rows of 8 heads of 128 channels in and out, two launches: 1 28.7 us, 2 21.4, 4 19.5,
+// 8 20.7; 85 MB, 13 us at the copy rate.)
+constexpr int kBatch = 4;
 
 // the least scale byte with 7 * scale >= amax (255 when none has)
 template <typename T> __device__ __forceinline__ uint32_t scale_byte(float amax)
