@@ -284,7 +284,7 @@ fedattn_status fedattn_decode_noalloc(const fedattn_shape *shape, int32_t mode,
  *     elements (multiples of 8, at least Hq*d / Hkv*d; 0 = packed): rows of a joint projection are read
  *     where they lie.  q or k may be NULL, together with its output: the other is done alone.
  *   q_weight, k_weight dev [d] in shape->dtype, or NULL (ones).  eps >= 0.  A row of zeros gives zeros
- *     when eps > 0.
+ *     when eps > 0.  Squares are summed in fp32: magnitudes stay below 2^60.
  *   pos dev int32 [n_rows], any value, or NULL (= row index).  inv_freq_host host double [rot_dim/2],
  *     finite, radians per position, read before the call returns (NULL when rot_dim == 0).
  *     rot_dim: multiple of 8, 0 .. d.

@@ -447,6 +447,10 @@ def _args_decode_window(ctx, shape, mode, q, k_cache, v_cache, cache_stride_part
                         lse, stream):
     n, dt = shape.n_participants, shape.torch_dtype
     rows = (n, shape.n_q_heads, shape.head_dim)
+    row = shape.n_kv_heads * shape.head_dim
+    held = int(max_kv_len) * row + (0 if int(mode) == DECODE_SYNC else (n - 1) * int(cache_stride_participant))
+    if min(k_cache.numel(), v_cache.numel()) < held:
+        raise ValueError("the caches have %d and %d elements, the call may read %d" % (k_cache.numel(), v_cache.numel(), held))
     return (ctx.handle, C.byref(shape), int(mode), _tensor(ctx, q, dt, rows, "q"),
             *[_tensor(ctx, t, dt, t.shape, "cache") for t in (k_cache, v_cache)], int(cache_stride_participant),
             _tensor(ctx, kv_len, torch.int32, (1 if int(mode) == DECODE_SYNC else n,), "kv_len"), int(max_kv_len), int(window),

@@ -35,6 +35,9 @@ inline float eff_scale(const fedattn_shape *s)
 
 inline int elt_bytes(const fedattn_shape *s) { return s->dtype == FEDATTN_BF16 ? 2 : 4; }
 
+// elements of a row of heads that are counted in 32 bits, at most
+constexpr int64_t kMostRow = 1 << 28;
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 PrefillParams prefill_params(const fedattn_shape *s, const void *q, const void *k, const void *v, void *o, float *lse,
@@ -431,6 +434,7 @@ fedattn_status fedattn_qk_norm_rope(fedattn_ctx *ctx, const fedattn_shape *shape
     if (!ctx || !shape_ok(shape) || n_rows < 0 || n_rows > 0x7fffffffLL) return FEDATTN_ERR_INVALID_ARG;
     if (!(eps >= 0.f) || isinf(eps) || (interleaved != 0 && interleaved != 1)) return FEDATTN_ERR_INVALID_ARG;
     const int d = shape->head_dim;
+    if (((int64_t)shape->n_q_heads + shape->n_kv_heads) * d > kMostRow) return FEDATTN_ERR_UNSUPPORTED;
     if (rot_dim < 0 || rot_dim > d || rot_dim % 8 != 0 || (rot_dim > 0 && !inv_freq_host)) return FEDATTN_ERR_INVALID_ARG;
     if (!q != !q_out || !k != !k_out) return FEDATTN_ERR_INVALID_ARG;
     RopeParams p;
@@ -472,7 +476,7 @@ fedattn_status quant_ok(const fedattn_ctx *ctx, const fedattn_shape *shape, int6
 {
     if (!ctx || !shape_ok(shape) || n_caches < 1 || cap < 0 || cap % 16 != 0) return FEDATTN_ERR_INVALID_ARG;
     if (cap > 0x7fffffffLL || n_caches > 0x7fffffffLL || n_caches * cap > 0x7fffffffLL) return FEDATTN_ERR_INVALID_ARG;
-    if (shape->head_dim % 32 != 0) return FEDATTN_ERR_UNSUPPORTED;
+    if (shape->head_dim % 32 != 0 || (int64_t)shape->n_kv_heads * shape->head_dim > kMostRow) return FEDATTN_ERR_UNSUPPORTED;
     if (cap > 0 && (!k_codes || !k_scales || !v_codes || !v_scales)) return FEDATTN_ERR_INVALID_ARG;
     if (!aligned16(k_codes) || !aligned16(k_scales) || !aligned16(v_codes) || !aligned16(v_scales)) return FEDATTN_ERR_INVALID_ARG;
     return FEDATTN_OK;

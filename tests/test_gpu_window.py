@@ -204,6 +204,8 @@ def test_what_is_refused():
         with pytest.raises(fa.FedAttnError):
             fa.fedattn_decode_window(ctx, shape, fa.DECODE_LOCAL, one, x, x, 0, length, 8, window, sink, one.clone())
     with pytest.raises(ValueError):
+        fa.fedattn_decode_window(ctx, shape, fa.DECODE_LOCAL, one, x, x[:7], 0, length, 8, 4, 0, one.clone())
+    with pytest.raises(ValueError):
         fa.fedattn_local_window(ctx, shape, x, x, x, [0, 7], 4, 0, x.clone())
     with pytest.raises(ValueError):
         fa.fedattn_local_window(ctx, shape, x.float(), x, x, [0, 8], 4, 0, x.clone())

@@ -82,6 +82,11 @@ def test_four_bit_caches_need_whole_groups(name, d):
     assert call(name, shape=bad_shape(head_dim=d)) == 2
 
 
+@pytest.mark.parametrize("name", ["fedattn_qk_norm_rope", "fedattn_quantize_kv", "fedattn_dequantize_kv", "fedattn_decode_quant"])
+def test_rows_that_are_not_counted_in_32_bits(name):
+    assert call(name, shape=bad_shape(n_q_heads=2 ** 31 - 1, n_kv_heads=2 ** 31 - 1)) == 2
+
+
 def test_workspace_too_small():
     assert call("fedattn_decode_quant") == 3      # the stand-in's workspace has no bytes
 
