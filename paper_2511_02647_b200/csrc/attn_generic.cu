@@ -459,7 +459,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
 #pragma unroll 1
     for (int r = rank; r < n_rows; r += plan.splits)
         if (s_bad[r] && (r / plan.splits) % (kThreads / 32) == warp)
-            attn_row_warp<T, true>(p, s_out[r] / p.hq, (int)(s_out[r] % p.hq), sQ + r * L::kQPitch);
+            attn_row_warp<T, true, kWindow>(p, s_out[r] / p.hq, (int)(s_out[r] % p.hq), sQ + r * L::kQPitch);
     if (plan.splits > 1) cluster.sync();                                     // peers may still be reading this CTA's partials
 }
 

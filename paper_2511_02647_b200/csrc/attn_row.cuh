@@ -20,8 +20,9 @@ template <> __device__ __forceinline__ void st_f<__nv_bfloat16>(__nv_bfloat16 *p
     *p = __float2bfloat16_rn(x);
 }
 
-// Called by a converged warp; q_s: d floats of shared memory of its own, which kQLoaded says hold the row of Q.
-template <typename T, bool kQLoaded = false>
+// Called by a converged warp; q_s: d floats of shared memory of its own, which kQLoaded says hold the row of Q.  kWindow: a local or
+// decode call through a window.
+template <typename T, bool kQLoaded, bool kWindow>
 __device__ __noinline__ void attn_row_warp(const GenericParams &p, int64_t row, int h, float *q_s)
 {
     const int lane = threadIdx.x & 31;
@@ -67,7 +68,7 @@ __device__ __noinline__ void attn_row_warp(const GenericParams &p, int64_t row, 
         test_pos = false;
     }
     int64_t win_lo = 0, win_hi = kv_hi, sink_hi = 0; // through a window: [win_lo, win_hi) and [kv_lo, sink_hi)
-    if (p.window > 0) {
+    if (kWindow) {
         const int n_keys = (int)(kv_hi - kv_lo);
         int i = n_keys - 1, len = n_keys;
         bool causal = true;
@@ -103,7 +104,7 @@ __device__ __noinline__ void attn_row_warp(const GenericParams &p, int64_t row, 
             const int64_t pj = kvp ? kvp[j] : j;
             ok = pj < own_lo || pj >= own_hi;
         }
-        if (p.window > 0) ok = ok && ((j >= win_lo && j < win_hi) || j < sink_hi);
+        if (kWindow) ok = ok && ((j >= win_lo && j < win_hi) || j < sink_hi);
         float s = -INFINITY;
         if (ok) {
             const T *kr = K + j * p.kv_tok_stride;

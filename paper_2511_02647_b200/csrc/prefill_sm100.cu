@@ -1439,7 +1439,7 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 __syncwarp();
 #pragma unroll 1
                 for (uint32_t left = bad; left; left &= left - 1) {
-                    attn_row_warp<__nv_bfloat16>(kp.row, sub.q_row0 + (r & ~31) + __ffs(left) - 1, sub.head,
+                    attn_row_warp<__nv_bfloat16, false, kWindow>(kp.row, sub.q_row0 + (r & ~31) + __ffs(left) - 1, sub.head,
                                                  reinterpret_cast<float *>(my_stage));
                     __syncwarp();
                 }
