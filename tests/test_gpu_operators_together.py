@@ -168,3 +168,28 @@ def test_sequences_without_synchronisation(dtype, d, hq, hkv, seed):
     for mode in ("free", "stream", "graph"):
         for i, (a, b) in enumerate(zip(sequence(dtype, d, hq, hkv, seed, mode), want)):
             assert torch.equal(a, b), (mode, i)
+
+
+def test_two_contexts_at_once_on_two_streams():
+    """Calls that overlap on the GPU share nothing but their inputs when each stream has a context of its own."""
+    n, hq, hkv, d, cap = 8, 32, 2, 128, 4096
+    shape = fa.Shape(n, hq, hkv, d, fa.BF16)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    cache = fa.QuantCache(shape, 1, cap, *[torch.randint(0, 256, (1, hkv, cap, w), dtype=torch.uint8, device="cuda", generator=gen) for w in (64, 4) * 2])
+    cache.k_scales.fill_(18 * 8)
+    cache.v_scales.fill_(18 * 8)
+    length = torch.tensor([cap], dtype=torch.int32, device="cuda")
+    qs = [torch.randn((n, hq, d), device="cuda", generator=gen).bfloat16() for _ in range(2)]
+    ctxs, streams = [fa.Context(shape, n, cap) for _ in range(2)], [torch.cuda.Stream() for _ in range(2)]
+    want = []
+    for c, q in zip(ctxs, qs):
+        want.append(torch.empty_like(q))
+        fa.fedattn_decode_quant(c, shape, fa.DECODE_SYNC, q, cache, length, cap, want[-1])
+        torch.cuda.synchronize()
+    outs = [[torch.empty_like(qs[0]) for _ in range(20)] for _ in range(2)]
+    for i in range(20):
+        for c, q, s, o in zip(ctxs, qs, streams, outs):
+            fa.fedattn_decode_quant(c, shape, fa.DECODE_SYNC, q, cache, length, cap, o[i], stream=s)
+    torch.cuda.synchronize()
+    for w, o in zip(want, outs):
+        assert all(torch.equal(w, x) for x in o)
