@@ -40,15 +40,24 @@ template <> __device__ __forceinline__ uint32_t codes_of<__nv_bfloat16>(float (&
     if (saturated)
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = fminf(fmaxf(x[e], -7.f * scale), 7.f * scale);
-    const float inv = 1.f / scale;
+    // (1 / scale to 2 units of the last place: t is off by 4e-6 at the most, far less than half a step of the first rounding)
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));
+    uint64_t t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        // to a multiple of 2^-13, then to an integer, plus 8, in the low bits of the sum
+        asm("{\n\t.reg .b64 x, c;\n\t"
+            "mov.b64 x, {%1, %2};\n\tmov.b64 c, {%3, %3};\n\tmul.rn.f32x2 x, x, c;\n\t"
+            "mov.b64 c, {%4, %4};\n\tadd.rn.f32x2 x, x, c;\n\tmov.b64 c, {%5, %5};\n\tadd.rn.f32x2 x, x, c;\n\t"
+            "mov.b64 c, {%6, %6};\n\tadd.rn.f32x2 %0, x, c;\n\t}"
+            : "=l"(t[i]) : "f"(x[2 * i]), "f"(x[2 * i + 1]), "f"(inv), "f"(1536.f), "f"(-1536.f), "f"(12582920.f));
+    }
+    // every sum's bits are 0x4b400000 + 8 + code: shifted and added without a mask, what the constants make is taken off at the end
     uint32_t w = 0;
 #pragma unroll
-    for (int e = 7; e >= 0; --e) {
-        // to a multiple of 2^-13, then to an integer in the low bits of the sum
-        const float t = __fadd_rn(__fadd_rn(__fmul_rn(x[e], inv), 1536.f), -1536.f);
-        w = w * 16 + (__float_as_uint(__fadd_rn(t, 12582920.f)) & 15u);
-    }
-    return w;
+    for (int i = 3; i >= 0; --i) w = (w * 16 + (uint32_t)(t[i] >> 32)) * 16 + (uint32_t)t[i];
+    return w - 0x4b400000u * 0x11111111u;
 }
 template <> __device__ __forceinline__ uint32_t codes_of<float>(float (&x)[8], float scale, bool)
 {

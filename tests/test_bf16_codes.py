@@ -13,10 +13,14 @@ def test_codes_of_every_value_under_every_scale():
         s = F(ref.SCALES[b])
         x = VALUES[VALUES <= 7 * s]
         x = np.concatenate([x, -x])
-        t = (x * (F(1) / s)).astype(F)
-        t = ((t + F(1536)).astype(F) - F(1536)).astype(F)                    # to a multiple of 2^-13
-        code = ((t + F(12582920)).astype(F).view(np.uint32) & 15).astype(np.int64) - 8
-        assert np.array_equal(code, np.rint(x.astype(np.float64) / ref.SCALES[b]).astype(np.int64)), b
+        want = np.rint(x.astype(np.float64) / ref.SCALES[b]).astype(np.int64)
+        inv = F(1) / s
+        for near in (inv, np.nextafter(inv, F(0)), np.nextafter(inv, F(1e30)), np.nextafter(np.nextafter(inv, F(0)), F(0)),
+                     np.nextafter(np.nextafter(inv, F(1e30)), F(1e30))):     # the reciprocal is an approximation
+            t = (x * near).astype(F)
+            t = ((t + F(1536)).astype(F) - F(1536)).astype(F)                # to a multiple of 2^-13
+            bits = (t + F(12582920)).astype(F).view(np.uint32)
+            assert np.array_equal(bits - np.uint32(0x4B400000), (want + 8).astype(np.uint32)), b
 
 
 def byte_of(amax):
