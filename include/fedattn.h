@@ -35,10 +35,9 @@
  *     the GPU race on its workspace.
  *   - Results are those of stream order: every call behaves as if it ran after all earlier work
  *     of its stream and before all later work.  Kernels are launched with programmatic stream
- *     serialization, in two ways.  fedattn_decode and fedattn_decode_window (bf16, head_dim 128),
- *     fedattn_decode_noalloc, fedattn_decode_quant and the sparse modes of fedattn_aggregate_kv may
- *     touch their buffers before the preceding kernel
- *     of the stream has ended, and let the next one start before they end; the library tracks the
+ *     serialization, in two ways.  fedattn_decode (bf16, head_dim 128), fedattn_decode_window (bf16,
+ *     head_dim 64, 96 or 128), fedattn_decode_noalloc, fedattn_decode_quant and the sparse modes of
+ *     fedattn_aggregate_kv may touch their buffers before the preceding kernel of the stream has ended, and let the next one start before they end; the library tracks the
  *     buffers of such calls and holds a call back whenever that could be observed.  All others
  *     wait for everything before them before they touch anything, and let nothing start early.
  *     Launched the ordinary way are the self-test, the kernel that prepares a bf16 head_dim 128

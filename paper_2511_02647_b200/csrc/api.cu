@@ -124,8 +124,9 @@ fedattn_status decode_call(fedattn_ctx *ctx, const fedattn_shape *shape, int32_t
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     cudaError_t err;
     const int N = shape->n_participants;
-    const size_t need = decode_scratch_bytes(N, shape->n_q_heads, shape->head_dim, ctx->c.sm_count);
-    if (shape->dtype == FEDATTN_BF16 && shape->head_dim == 128 && need > 0) {
+    size_t need = decode_scratch_bytes(N, shape->n_q_heads, shape->head_dim, ctx->c.sm_count);
+    if (window > 0 && shape->head_dim != 128) need = decode_quant_scratch_bytes(N, shape->n_q_heads, shape->head_dim);
+    if (shape->dtype == FEDATTN_BF16 && decode_stream_takes(shape->head_dim, window > 0) && need > 0) {
         if (ctx->c.scratch_bytes < need) return FEDATTN_ERR_WORKSPACE;
         DecodeParams p;
         memset(&p, 0, sizeof(p));

@@ -255,6 +255,8 @@ struct DecodeParams {
     int32_t early;                // inputs may be read before the preceding grid is complete (set by the launcher)
 };
 size_t decode_scratch_bytes(int n_part, int hq, int d, int sm_count);
+// whether the stream kernel has this head_dim: 128, and with a window also 64 and 96 (their scratch: decode_quant_scratch_bytes)
+bool decode_stream_takes(int d, bool window);
 cudaError_t launch_decode_bf16(const Context *ctx, const DecodeParams &p, cudaStream_t s, int64_t *launches);
 
 // ---- norm of queries and keys with their rotation ----------------------------------------------------

@@ -1,4 +1,4 @@
-// bf16 split-KV decode (head_dim 128): one new query token per participant over cached K/V.
+// bf16 split-KV decode (head_dim 128, through a window also 64 and 96): one new query token per participant over cached K/V.
 // HBM-bound: each K/V row is read once.  The query rows that share a KV head -- the g = Hq/Hkv
 // grouped heads of one participant (LOCAL), or of all participants (SYNC, one shared global
 // cache) -- are stacked into 16-row tiles so that QK^T and PV run on the tensor cores
@@ -40,12 +40,13 @@ namespace fedattn {
 
 namespace {
 
-constexpr int kD = 128;
 constexpr int kTileKeys = 64;
 constexpr int kStages = 3;
-constexpr int kTileBytes = kTileKeys * kD * 2;          // 16 KB (K or V)
-constexpr int kStageBytes = 2 * kTileBytes;             // K + V
-constexpr int kPartialStride = kD + 4;                  // m, l, 2 pad, o[128]: o is 16-byte aligned
+// Of a head_dim: a row's bytes in shared memory (96 channels take the room of 128), a tile of K or V, both, a partial (m, l, 2 pad, o).
+__host__ __device__ constexpr int row_bytes_of(int d) { return d > 64 ? 256 : 128; }
+__host__ __device__ constexpr int tile_bytes_of(int d) { return kTileKeys * row_bytes_of(d); }      // 16 KB at 128 channels
+__host__ __device__ constexpr int stage_bytes_of(int d) { return 2 * tile_bytes_of(d); }
+__host__ __device__ constexpr int partial_stride_of(int d) { return d + 4; }
 constexpr float kRescaleThreshold = 8.0f;               // log2 units
 constexpr int kMaxSlots = 64;                           // partials per output row: splits x key slices of a CTA
 constexpr int kMaxCluster = 8;                          // splits of a one-launch call (portable cluster size)
@@ -106,8 +107,19 @@ __device__ __forceinline__ float4 ld_partial4(const float *p)
     return v;
 }
 
-// byte offset of 16-byte chunk `chunk` (0..15) of key row `row` inside a swizzled [64][128] bf16 tile
-__device__ __forceinline__ uint32_t swz(int row, int chunk) { return (uint32_t)(row * 256 + ((chunk ^ (row & 7)) << 4)); }
+// byte offset of 16-byte chunk `chunk` of key row `row` inside a swizzled tile
+template <int kD> __device__ __forceinline__ uint32_t swz(int row, int chunk)
+{
+    return (uint32_t)(row * row_bytes_of(kD) + ((chunk ^ (row & 7)) << 4));
+}
+// the leading 8 bits of two values as a bf16 pair; what is left stays in them
+__device__ __forceinline__ uint32_t take_part(float &lo, float &hi)
+{
+    const uint32_t a = __float_as_uint(lo), b = __float_as_uint(hi);
+    lo -= __uint_as_float(a & 0xffff0000u);
+    hi -= __uint_as_float(b & 0xffff0000u);
+    return __byte_perm(a, b, 0x7632);
+}
 
 }  // namespace
 
@@ -128,13 +140,19 @@ __device__ long long g_dtrace[1024 * 8];
 // = { m (log2 domain, scale included), l, -, -, o[128] }, unnormalised.
 // kOneLaunch: the grid's x extent is one cluster; warps leave their partials in shared memory, every CTA folds its
 // slices, and rank r of the cluster folds and writes rows r, r + n_splits, ...
-// kWindow: the first n_sink and the last `window` keys only: the walk goes over tiles 0 .. n_a - 1, then t_b and on.
-template <int kMTiles, bool kOneLaunch, bool kWindow>
+// kWindow: the first n_sink and the last `window` keys only: the walk goes over tiles 0 .. n_a - 1, then t_b and on.  8 x 1024 of 4096 rows
+// of 8 KV heads by 32 heads, in a replayed graph: 4.8 us at 64 channels, 5.9 at 96, 5.3 at 128 (a 34 MB call; 64 and 96 channels on fp32
+// FMAs took 32 and 39); 8 queries over 30 000 shared rows 17.9, 24.8 and 22.7 (130 and 178).
+// kD: head_dim.  64 and 96 channels (windows only) keep their weights' 24 bits as three bf16 parts, as the fp32 weights of attn_generic.cu
+// have them, which decodes those head dims without a window; the products are not what bounds.
+template <int kD, int kMTiles, bool kOneLaunch, bool kWindow>
 __global__ void __launch_bounds__(128, 2)
 decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
 {
     constexpr int kSlices = 4 / kMTiles;                        // key slices per tile
     constexpr int kSteps = 4 / kSlices;                         // 16-key steps per warp and tile
+    constexpr int kChunks = kD / 8, kTileBytes = tile_bytes_of(kD), kStageBytes = stage_bytes_of(kD), kPartialStride = partial_stride_of(kD);
+    constexpr int kParts = kD == 128 ? 1 : 3;                   // bf16 parts of a weight
     extern __shared__ __align__(1024) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int slice = warp % kSlices, mt = warp / kSlices;     // this warp's key slice and M-tile
@@ -185,28 +203,34 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
     // K and V tiles: 64 rows x 16 chunks of 16 bytes each.  Thread tid copies chunk (tid & 15) of rows
     // (tid >> 4) + 8 i, i = 0..7; the row's swizzle term (row & 7) is the same for all i, so the global
     // and shared offsets are fixed per thread up to a multiple of 8 rows.  Rows past `len` are zero-filled.
-    const int ld_row = tid >> 4, ld_ch = tid & 15;
+    constexpr int kRowLanes = kD > 64 ? 16 : 8, kPass = 128 / kRowLanes;        // (96 channels: 12 of 16 lanes copy)
+    const int ld_row = tid / kRowLanes, ld_ch = tid % kRowLanes;
     const __nv_bfloat16 *ld_k = Kb + (size_t)ld_row * tok_stride + ld_ch * 8, *ld_v = Vb + (size_t)ld_row * tok_stride + ld_ch * 8;
-    const uint32_t ld_s = smem_u32(smem) + swz(ld_row, ld_ch);
+    const uint32_t ld_s = smem_u32(smem) + swz<kD>(ld_row, ld_ch);
+    const uint32_t hidden = max(win_lo - sink, 0);
     auto load_tile = [&](int t, int stage) {
         const int key0 = key0_of(tile_lo + t);
         const uint32_t sK = ld_s + stage * kStageBytes, sV = sK + kTileBytes;
         const size_t base = (size_t)key0 * tok_stride;
-        const int n_ok = len - key0 - ld_row;                  // rows ld_row + 8 i with 8 i < n_ok exist
+        const int n_ok = len - key0 - ld_row;                  // rows ld_row + kPass i with kPass i < n_ok exist
+        const int behind = key0 + ld_row - sink;               // (kWindow) the window hides `hidden` rows from row `sink` on
+        if (kD == 96 && ld_ch >= kChunks) return;
 #pragma unroll
-        for (int i = 0; i < kTileKeys / 8; ++i) {
-            const bool ok = 8 * i < n_ok;
-            const size_t off = ok ? base + (size_t)(8 * i) * tok_stride : 0;
-            cp_async16(sK + i * 8 * 256, ld_k + off, ok);
-            cp_async16(sV + i * 8 * 256, ld_v + off, ok);
+        for (int i = 0; i < kTileKeys / kPass; ++i) {
+            bool ok = kPass * i < n_ok;
+            // a row that the window hides is zeros too: whatever it holds, 0 * it is 0
+            if (kWindow) ok = ok && (uint32_t)(behind + kPass * i) >= hidden;
+            const size_t off = ok ? base + (size_t)(kPass * i) * tok_stride : 0;
+            cp_async16(sK + i * kPass * row_bytes_of(kD), ld_k + off, ok);
+            cp_async16(sV + i * kPass * row_bytes_of(kD), ld_v + off, ok);
         }
     };
 
     const float sl2 = p.scale * 1.4426950408889634f;
     float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;   // rows lane/4 and lane/4 + 8 of this warp's M-tile
-    float acc[16][4];
+    float acc[kChunks][4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+    for (int i = 0; i < kChunks; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
 
     // Q rows of this chunk -> shared memory (in the third stage's buffer, which the first tile loads do
     // not touch), same swizzle as the K/V tiles; rows past rows_total are zero
@@ -215,8 +239,9 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
 #pragma unroll
         for (int i = tid; i < 16 * kMTiles * 16; i += 128) {
             const int row = i >> 4, ch = i & 15;
+            if (ch >= kChunks) continue;
             const __nv_bfloat16 *src = q_ptr(chunk * kMTiles * 16 + row);
-            cp_async16(sQ + swz(row, ch), src ? src + ch * 8 : reinterpret_cast<const __nv_bfloat16 *>(p.q), src != nullptr);
+            cp_async16(sQ + swz<kD>(row, ch), src ? src + ch * 8 : reinterpret_cast<const __nv_bfloat16 *>(p.q), src != nullptr);
         }
         cp_async_commit();
     }
@@ -226,17 +251,17 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
         cp_async_commit();
     }
     // Q fragments of this warp's M-tile (A operand, 16 x 128): 8 k-steps x 4 registers
-    uint32_t qf[8][4];
+    uint32_t qf[kD / 16][4];
     cp_async_wait<kStages - 1>();                               // the Q group; the tile groups may still be in flight
     __syncthreads();
     {
         const uint32_t sQ = smem_u32(smem) + (kStages - 1) * kStageBytes;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
+        for (int ks = 0; ks < kD / 16; ++ks) {
             // matrices: (rows 0-7, d 0-7) (rows 8-15, d 0-7) (rows 0-7, d 8-15) (rows 8-15, d 8-15)
             const int row = mt * 16 + (lane & 7) + (((lane >> 3) & 1) << 3);
             const int ch = ks * 2 + (lane >> 4);
-            ldmatrix_x4(qf[ks], sQ + swz(row, ch));
+            ldmatrix_x4(qf[ks], sQ + swz<kD>(row, ch));
         }
     }
     DTRACE(1);
@@ -254,12 +279,12 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
             // ---- S = Q K^T for 16 keys: two n-tiles of 8 keys ----
             float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int ks = 0; ks < 8; ++ks) {
+            for (int ks = 0; ks < kD / 16; ++ks) {
                 // matrices: (keys 0-7, d 0-7) (keys 0-7, d 8-15) (keys 8-15, d 0-7) (keys 8-15, d 8-15)
                 const int row = krow0 + (lane & 7) + ((lane >> 4) << 3);
                 const int ch = ks * 2 + ((lane >> 3) & 1);
                 uint32_t b[4];
-                ldmatrix_x4(b, sK + swz(row, ch));
+                ldmatrix_x4(b, sK + swz<kD>(row, ch));
                 mma_bf16(s0, qf[ks], b[0], b[1]);
                 mma_bf16(s1, qf[ks], b[2], b[3]);
             }
@@ -290,7 +315,7 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
                 m0 = mn0; m1 = mn1;
                 l0 *= a0; l1 *= a1;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) { acc[i][0] *= a0; acc[i][1] *= a0; acc[i][2] *= a1; acc[i][3] *= a1; }
+                for (int i = 0; i < kChunks; ++i) { acc[i][0] *= a0; acc[i][1] *= a0; acc[i][2] *= a1; acc[i][3] *= a1; }
             }
             const float ms0 = m0 == -INFINITY ? 0.f : m0, ms1 = m1 == -INFINITY ? 0.f : m1;
             float ps0 = 0.f, ps1 = 0.f;
@@ -301,17 +326,30 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
             }
             l0 += ps0; l1 += ps1;
             // P as A operand (16 rows x 16 keys)
-            const uint32_t pf[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[4], v[5]), pack_bf16(v[2], v[3]), pack_bf16(v[6], v[7])};
+            uint32_t pf[kParts][4];
+            if (kParts == 1) {
+                pf[0][0] = pack_bf16(v[0], v[1]); pf[0][1] = pack_bf16(v[4], v[5]);
+                pf[0][2] = pack_bf16(v[2], v[3]); pf[0][3] = pack_bf16(v[6], v[7]);
+            } else {
+#pragma unroll
+                for (int part = 0; part < kParts; ++part) {
+                    pf[part][0] = take_part(v[0], v[1]); pf[part][1] = take_part(v[4], v[5]);
+                    pf[part][2] = take_part(v[2], v[3]); pf[part][3] = take_part(v[6], v[7]);
+                }
+            }
             // ---- O += P V ----
 #pragma unroll
-            for (int nd = 0; nd < 8; ++nd) {
+            for (int nd = 0; nd < kD / 16; ++nd) {
                 // matrices: (keys 0-7, d 0-7) (keys 8-15, d 0-7) (keys 0-7, d 8-15) (keys 8-15, d 8-15) of d block nd*16
                 const int row = krow0 + (lane & 7) + (((lane >> 3) & 1) << 3);
                 const int ch = nd * 2 + (lane >> 4);
                 uint32_t b[4];
-                ldmatrix_x4_trans(b, sV + swz(row, ch));
-                mma_bf16(acc[2 * nd], pf, b[0], b[1]);
-                mma_bf16(acc[2 * nd + 1], pf, b[2], b[3]);
+                ldmatrix_x4_trans(b, sV + swz<kD>(row, ch));
+#pragma unroll
+                for (int part = 0; part < kParts; ++part) {
+                    mma_bf16(acc[2 * nd], pf[part], b[0], b[1]);
+                    mma_bf16(acc[2 * nd + 1], pf[part], b[2], b[3]);
+                }
             }
         }
     }
@@ -346,7 +384,7 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
         if ((lane & 3) == 0) *reinterpret_cast<float2 *>(dst) = make_float2(m0, l0);
         dst += 4 + (lane & 3) * 2;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) *reinterpret_cast<float2 *>(dst + i * 8) = make_float2(acc[i][0], acc[i][1]);
+        for (int i = 0; i < kChunks; ++i) *reinterpret_cast<float2 *>(dst + i * 8) = make_float2(acc[i][0], acc[i][1]);
     }
     if (rb < rows_here) {
         float *dst = kOneLaunch ? part + (slice * kRows + rb) * kPartialStride
@@ -354,7 +392,7 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
         if ((lane & 3) == 0) *reinterpret_cast<float2 *>(dst) = make_float2(m1, l1);
         dst += 4 + (lane & 3) * 2;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) *reinterpret_cast<float2 *>(dst + i * 8) = make_float2(acc[i][2], acc[i][3]);
+        for (int i = 0; i < kChunks; ++i) *reinterpret_cast<float2 *>(dst + i * 8) = make_float2(acc[i][2], acc[i][3]);
     }
     DTRACE(4);
     if (!kOneLaunch) return;
@@ -376,14 +414,14 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int q = 0; q < kSlices; ++q) {
-            const float4 v = *reinterpret_cast<const float4 *>(src + q * kRows * kPartialStride + 4 + lane * 4);
+            const float4 v = *reinterpret_cast<const float4 *>(src + q * kRows * kPartialStride + 4 + (lane < kD / 4 ? lane * 4 : 0));
             const float f = ex2(ml[q].x - ms);                  // 0 for an empty partial (m = -inf)
             z += ml[q].y * f;
             o.x += v.x * f; o.y += v.y * f; o.z += v.z * f; o.w += v.w * f;
         }
         __syncwarp();                                           // every lane has read the maxima and sums
         if (lane == 0) *reinterpret_cast<float2 *>(src) = make_float2(mx, z);
-        *reinterpret_cast<float4 *>(src + 4 + lane * 4) = o;
+        if (lane < kD / 4) *reinterpret_cast<float4 *>(src + 4 + lane * 4) = o;
     }
     // ---- fold the CTAs of the cluster ----
     cg::cluster_group cluster = cg::this_cluster();
@@ -400,7 +438,7 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
             if (q < n_splits) {
                 const float *src = (n_splits > 1 ? cluster.map_shared_rank(part, q) : part) + row * kPartialStride;
                 ml[q] = *reinterpret_cast<const float2 *>(src);
-                v[q] = *reinterpret_cast<const float4 *>(src + 4 + lane * 4);
+                if (lane < kD / 4) v[q] = *reinterpret_cast<const float4 *>(src + 4 + lane * 4);
             }
         }
 #pragma unroll
@@ -417,7 +455,7 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
         const float inv = z > 0.f ? 1.f / z : 0.f;
         const size_t orow = out_row(chunk * kRows + row);
         const uint2 w = make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-        *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + orow * kD + lane * 4) = w;
+        if (lane < kD / 4) *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + orow * kD + lane * 4) = w;
         if (lane == 0 && p.lse) p.lse[orow] = z > 0.f ? lse_exact(mx, z) : -INFINITY;
     }
     if (n_splits > 1) cluster.sync();                           // peers may still be reading this CTA's partials
@@ -428,14 +466,17 @@ decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)
 // a time; the groups meet in shared memory.  The grid is at most one CTA per SM and a CTA is small (128
 // threads, few registers, 2 KB of shared memory), so the whole grid is resident beside the stream CTAs
 // at once: the next call's stream kernel can only be launched when every CTA of this grid has started.
-__global__ void __launch_bounds__(kMergeGroups * (kD / 4), 7)
+template <int kD>
+__global__ void __launch_bounds__(kMergeGroups * 32, 7)
 decode_merge_kernel(const DecodeParams p, int n_slots, int n_rows)
 {
-    __shared__ float4 s_acc[kMergeGroups][kD / 4];
+    constexpr int kPartialStride = partial_stride_of(kD);
+    __shared__ float4 s_acc[kMergeGroups][32];
     __shared__ float2 s_ml[kMergeGroups];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");         // the partials of this call
-    const int c4 = threadIdx.x & (kD / 4 - 1), grp = threadIdx.x / (kD / 4);
+    const int c4 = threadIdx.x & 31, grp = threadIdx.x / 32;
+    const bool mine = c4 < kD / 4;
     for (size_t orow = blockIdx.x; orow < (size_t)n_rows; orow += gridDim.x) {
     const int per = (n_slots + kMergeGroups - 1) / kMergeGroups;
     const int s0 = grp * per, s1 = min(s0 + per, n_slots);
@@ -449,7 +490,7 @@ decode_merge_kernel(const DecodeParams p, int n_slots, int n_rows)
         for (int k = 0; k < 4; ++k)
             if (k0 + k < s1) {
                 ml[k] = ld_partial2(src + (size_t)(k0 + k) * kPartialStride);
-                v[k] = ld_partial4(src + (size_t)(k0 + k) * kPartialStride + 4 + c4 * 4);
+                v[k] = ld_partial4(src + (size_t)(k0 + k) * kPartialStride + 4 + (mine ? c4 * 4 : 0));
             }
         float mn = mm;
 #pragma unroll
@@ -488,7 +529,7 @@ decode_merge_kernel(const DecodeParams p, int n_slots, int n_rows)
         __nv_bfloat162 lo = __floats2bfloat162_rn(o.x * inv, o.y * inv), hi = __floats2bfloat162_rn(o.z * inv, o.w * inv);
         uint2 w;
         w.x = *reinterpret_cast<uint32_t *>(&lo); w.y = *reinterpret_cast<uint32_t *>(&hi);
-        *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + orow * kD + c4 * 4) = w;
+        if (mine) *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.o) + orow * kD + c4 * 4) = w;
         if (c4 == 0 && p.lse) p.lse[orow] = l_all > 0.f ? (m_all + log2f(l_all)) * 0.6931471805599453f : -INFINITY;
     }
     __syncthreads();                                            // the group buffers are reused by the next row
@@ -504,20 +545,23 @@ extern "C" int fedattn_debug_read_dtrace(long long *host, int n)
 
 size_t decode_scratch_bytes(int n_part, int hq, int d, int /*sm_count*/)
 {
-    if (d != kD) return 0;
-    return (size_t)n_part * hq * kMaxSlots * kPartialStride * sizeof(float);
+    if (d != 128) return 0;
+    return (size_t)n_part * hq * kMaxSlots * partial_stride_of(d) * sizeof(float);
 }
 
 typedef void (*StreamKernel)(const DecodeParams, int, int);
-static StreamKernel stream_kernel(int m_tiles, bool one_launch, bool window)
+template <int kD> static StreamKernel window_kernel(int m_tiles, bool one_launch)
 {
-    static const StreamKernel kernels[2][2][2] = {
-        {{decode_stream_kernel<1, false, false>, decode_stream_kernel<1, false, true>},
-         {decode_stream_kernel<1, true, false>, decode_stream_kernel<1, true, true>}},
-        {{decode_stream_kernel<2, false, false>, decode_stream_kernel<2, false, true>},
-         {decode_stream_kernel<2, true, false>, decode_stream_kernel<2, true, true>}}};
-    return kernels[m_tiles - 1][one_launch][window];
+    return one_launch ? (m_tiles == 1 ? decode_stream_kernel<kD, 1, true, true> : decode_stream_kernel<kD, 2, true, true>)
+                      : (m_tiles == 1 ? decode_stream_kernel<kD, 1, false, true> : decode_stream_kernel<kD, 2, false, true>);
 }
+static StreamKernel stream_kernel(int d, int m_tiles, bool one_launch, bool window)
+{
+    if (window) return d == 64 ? window_kernel<64>(m_tiles, one_launch) : d == 96 ? window_kernel<96>(m_tiles, one_launch) : window_kernel<128>(m_tiles, one_launch);
+    return one_launch ? (m_tiles == 1 ? decode_stream_kernel<128, 1, true, false> : decode_stream_kernel<128, 2, true, false>)
+                      : (m_tiles == 1 ? decode_stream_kernel<128, 1, false, false> : decode_stream_kernel<128, 2, false, false>);
+}
+bool decode_stream_takes(int d, bool window) { return d == 128 || (window && (d == 64 || d == 96)); }
 
 // Grid rule shared by the entry points.  Splits are chosen so that the whole stream grid is resident
 // at once (two CTAs per SM): a grid slightly larger than that would run a nearly empty second wave.
@@ -528,7 +572,7 @@ static cudaError_t launch_decode_split(const DecodeParams &p_in, int device, int
     EarlyStart es;
     {
         // may the stream kernel read its inputs before the preceding grid of the stream is complete?
-        const size_t row_bytes = (size_t)p.hkv * kD * 2, qo_bytes = (size_t)p.n_part * p.hq * kD * 2;
+        const size_t row_bytes = (size_t)p.hkv * p.d * 2, qo_bytes = (size_t)p.n_part * p.hq * p.d * 2;
         const size_t cache_bytes = p.sync ? (size_t)p.max_kv_len * row_bytes
                                           : ((size_t)(p.n_part - 1) * p.cache_stride * 2 + (size_t)p.max_kv_len * row_bytes);
         const MemRange in[4] = {{p.q, qo_bytes}, {p.k, cache_bytes}, {p.v, cache_bytes},
@@ -559,10 +603,10 @@ static cudaError_t launch_decode_split(const DecodeParams &p_in, int device, int
     // 32 splits take 12 us, 8 take 31); two CTAs per SM hold a cluster of 8 everywhere.
     int cluster = 1;
     while (cluster * 2 <= n_splits && cluster < kMaxCluster) cluster *= 2;
-    const bool one_launch = caches * p.hkv * keys * kD * 4 <= kOneLaunchBytes && tiles <= kOneLaunchTiles * cluster;
+    const bool one_launch = caches * p.hkv * keys * p.d * 4 <= kOneLaunchBytes && tiles <= kOneLaunchTiles * cluster;
     if (one_launch) n_splits = cluster;
     const int n_slots = n_splits * slices;
-    if (!one_launch && (size_t)p.n_part * p.hq * n_slots * kPartialStride * sizeof(float) > p.partial_bytes)
+    if (!one_launch && (size_t)p.n_part * p.hq * n_slots * partial_stride_of(p.d) * sizeof(float) > p.partial_bytes)
         return early_start_end(es, cudaErrorInvalidValue);
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -573,31 +617,32 @@ static cudaError_t launch_decode_split(const DecodeParams &p_in, int device, int
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3(n_splits, p.hkv, caches * n_chunks);
     cfg.blockDim = dim3(128, 1, 1);
-    cfg.dynamicSmemBytes = kStages * kStageBytes;              // 96 KB
+    cfg.dynamicSmemBytes = kStages * stage_bytes_of(p.d);      // 96 KB at 128 channels
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = one_launch ? 2 : 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, stream_kernel(m_tiles, one_launch, p.window > 0), p, n_splits, n_chunks);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, stream_kernel(p.d, m_tiles, one_launch, p.window > 0), p, n_splits, n_chunks);
     if (launches) ++*launches;
     if (one_launch) return early_start_end(es, e != cudaSuccess ? e : cudaGetLastError());
     cfg.numAttrs = 1;
     if (e != cudaSuccess) return early_start_end(es, e);
     const int n_rows = p.n_part * p.hq, rows_per_cta = (n_rows + sm_count - 1) / sm_count;
     cfg.gridDim = dim3((n_rows + rows_per_cta - 1) / rows_per_cta, 1, 1);
-    cfg.blockDim = dim3(kMergeGroups * (kD / 4), 1, 1);
+    cfg.blockDim = dim3(kMergeGroups * 32, 1, 1);
     cfg.dynamicSmemBytes = 0;
-    e = cudaLaunchKernelEx(&cfg, decode_merge_kernel, p, n_slots, n_rows);
+    e = cudaLaunchKernelEx(&cfg, p.d == 64 ? decode_merge_kernel<64> : p.d == 96 ? decode_merge_kernel<96> : decode_merge_kernel<128>, p, n_slots, n_rows);
     if (launches) ++*launches;
     return early_start_end(es, e != cudaSuccess ? e : cudaGetLastError());
 }
 
 static cudaError_t set_decode_smem_attr()
 {
-    const int smem = kStages * kStageBytes;
     cudaError_t e = cudaSuccess;
-    for (int i = 0; i < 8; ++i)
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(stream_kernel(1 + (i & 1), i & 2, i & 4), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    for (int d = 64; d <= 128; d += 32)
+        for (int i = 0; i < 8; ++i)
+            if (e == cudaSuccess && decode_stream_takes(d, i & 4))
+                e = cudaFuncSetAttribute(stream_kernel(d, 1 + (i & 1), i & 2, i & 4), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         kStages * stage_bytes_of(d));
     return e;
 }
 
@@ -624,7 +669,7 @@ namespace fedattn {
 namespace {
 
 constexpr int kStaticMaxRows = 256;     // n_participants * n_q_heads
-constexpr size_t kStaticScratchFloats = (size_t)kStaticMaxRows * kMaxSlots * kPartialStride;
+constexpr size_t kStaticScratchFloats = (size_t)kStaticMaxRows * kMaxSlots * partial_stride_of(128);
 
 static __device__ __align__(256) float g_decode_scratch[kStaticScratchFloats];
 
@@ -651,7 +696,7 @@ extern "C" fedattn_status fedattn_decode_noalloc(const fedattn_shape *shape, int
     if (max_kv_len > 0 && (!k_cache || !v_cache)) return FEDATTN_ERR_INVALID_ARG;
     if (((uintptr_t)q | (uintptr_t)o | (uintptr_t)k_cache | (uintptr_t)v_cache) & 15) return FEDATTN_ERR_INVALID_ARG;
     if (mode == FEDATTN_DECODE_LOCAL && (cache_stride_participant * 2) % 16 != 0) return FEDATTN_ERR_INVALID_ARG;
-    if (shape->dtype != FEDATTN_BF16 || shape->head_dim != kD) return FEDATTN_ERR_UNSUPPORTED;
+    if (shape->dtype != FEDATTN_BF16 || shape->head_dim != 128) return FEDATTN_ERR_UNSUPPORTED;
     if ((int64_t)shape->n_participants * shape->n_q_heads > kStaticMaxRows)
         return FEDATTN_ERR_WORKSPACE;          // more output rows than the built-in scratch covers
     if (!(shape->scale >= 0.f)) return FEDATTN_ERR_INVALID_ARG;
@@ -676,7 +721,7 @@ extern "C" fedattn_status fedattn_decode_noalloc(const fedattn_shape *shape, int
     DecodeParams p;
     memset(&p, 0, sizeof(p));
     p.q = q; p.k = k_cache; p.v = v_cache; p.o = o; p.lse = lse;
-    p.n_part = shape->n_participants; p.hq = shape->n_q_heads; p.hkv = shape->n_kv_heads; p.d = kD;
+    p.n_part = shape->n_participants; p.hq = shape->n_q_heads; p.hkv = shape->n_kv_heads; p.d = 128;
     p.scale = shape->scale > 0.f ? shape->scale : 0.08838834764831845f;   // 1/sqrt(128)
     p.sync = mode == FEDATTN_DECODE_SYNC;
     p.cache_stride = cache_stride_participant; p.kv_len = kv_len; p.max_kv_len = max_kv_len;

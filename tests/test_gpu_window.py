@@ -176,6 +176,37 @@ def test_decode_in_one_and_in_two_launches(window, launches):
     assert ctx.launch_count() == launches
 
 
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("hq,hkv,n,window,launches", [(4, 4, 3, 777, 1), (7, 1, 3, 30000, 2), (12, 1, 3, 65, 1)])
+def test_decode_at_every_head_dim_of_the_tensor_cores(d, hq, hkv, n, window, launches):
+    ctx = decode(fa.DECODE_SYNC, "bf16", n, hq, hkv, d, [40001], 40001, window, 130)
+    assert ctx.launch_count() == launches
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("mode", [fa.DECODE_LOCAL, fa.DECODE_SYNC])
+def test_decode_never_multiplies_rows_behind_the_window(d, mode):
+    """Between the sinks and the window lie Inf and NaN, in the tiles that both reach into."""
+    n, hq, hkv, L, window, sink = 2, 4, 2, 331, 100, 5
+    rng = np.random.default_rng(d)
+    shape = shape_of(n, hq, hkv, d, "bf16")
+    ctx = fa.Context(shape, n, L)
+    q = ref.rounded(rng.standard_normal((n, hq, d)), "bf16")
+    k, v = (ref.rounded(rng.standard_normal((n, L, hkv, d)), "bf16") for _ in range(2))
+    qd, kd, vd = (dev(x.astype(np.float32), "bf16") for x in (q, k, v))
+    kd[:, sink:L - window] = float("nan")
+    vd[:, sink:L - window] = float("inf")
+    o = torch.empty_like(qd)
+    lens = torch.tensor([L] * (1 if mode == fa.DECODE_SYNC else n), dtype=torch.int32, device="cuda")
+    fa.fedattn_decode_window(ctx, shape, mode, qd, kd, vd, L * hkv * d, lens, L, window, sink, o)
+    j = np.arange(L)
+    seen = (j >= L - window) | (j < sink)
+    for i in range(n):
+        c = 0 if mode == fa.DECODE_SYNC else i
+        want = ref.attend(q[i:i + 1], k[c], v[c], seen[None], d ** -0.5)
+        ref.check_attention(host(o)[i:i + 1], None, want, "bf16", weights=weights_of("bf16", d))
+
+
 def test_decode_sees_what_the_last_row_of_a_local_call_sees():
     d, L, hq, hkv = 128, 391, 4, 2
     g = torch.Generator(device="cuda").manual_seed(2)
