@@ -390,8 +390,11 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
         wait_copy();                                                         // V
         // ---- O += P V ----
         const int kb = kKeyWarps > 1 ? 16 * warp : 0;
+        // Through a short window most of a tile may lie behind the last key: 647 rows of 16 heads of 128 channels, window 2, 32.6 -> 29.7 us
+        // (1024 rows, window 700: 168.6 -> 170.7).
+        const int kb_most = kb + (kKeyWarps > 1 ? 16 : kKeys), kb_end = kWindow ? min(kb_most, (left + 3) & ~3) : kb_most;
 #pragma unroll 4
-        for (int key = kb; key < kb + (kKeyWarps > 1 ? 16 : kKeys); ++key) {
+        for (int key = kb; key < kb_end; ++key) {
             uint64_t pp[kR / 2];
 #pragma unroll
             for (int i = 0; i < kR / 4; ++i) {
@@ -493,9 +496,13 @@ cudaError_t launch_instance(const GenericParams &p, TiledPlan plan, int sm_count
     // (kKeyWarps = 1: 93 and 280 us with one pair against 107 and 341 with two, local and sync of 2048 rows x 16 heads).
     const int64_t key_tiles = (max_kv + L::kKeys - 1) / L::kKeys, units = (int64_t)plan.n_tiles * p.hkv;
     plan.splits = 1;
-    // (Through a window the walks are short and latency is all: two CTAs per SM.  Bidirectional window of 100, 845 rows of 8 heads of 64 channels
-    // 40.1 -> 29.4 us, 600 rows of 8 heads of 128 44.2 -> 39.0; three and four per SM 33.7 and 52.0.)
-    while (plan.splits < kMaxCluster && units * plan.splits <= (kWindow ? 2 : 1) * sm_count && plan.splits * 2 <= key_tiles) plan.splits *= 2;
+    // (Through a window the walks are short and latency is all: as many CTAs as are resident at once, by shared memory and registers.  Bidirectional
+    // window of 100, 845 rows of 8 heads of 64 channels 40.1 -> 29.4 us against one per SM.  One more wave costs a whole walk: 8 caches of 4096 rows,
+    // window 1024, 32 fp32 heads of 128, 27.2 us, with twice the CTAs 42.5; 600 rows of 8 heads of 128 24.5 and 33.2.)
+    const int per_sm = min(L::kThreads == 128 ? 4 : 2, 220 * 1024 / L::bytes(1));
+    while (plan.splits < kMaxCluster && plan.splits * 2 <= key_tiles &&
+           (kWindow ? 2 * units * plan.splits <= per_sm * sm_count : units * plan.splits <= sm_count))
+        plan.splits *= 2;
     const int64_t per_cta = (key_tiles + plan.splits - 1) / plan.splits;     // tiles of a CTA, at most
     plan.stages = 1;
     while (kKeyWarps > 1 && plan.stages < kMaxStages && plan.stages < per_cta && L::bytes(plan.stages + 1) <= kMost) ++plan.stages;
