@@ -343,7 +343,9 @@ fedattn_status fedattn_decode_quant(fedattn_ctx *ctx, const fedattn_shape *shape
  *                        sync block of a windowed model) is this call with one participant.
  * fedattn_decode_window  as fedattn_decode, but only the last `window` of the kv_len cached rows and the first
  *                        n_sink.  With the new token's own row cached before the call it sees what the same
- *                        row of fedattn_local_window sees.
+ *                        row of fedattn_local_window sees.  bf16 with head_dim 64, 96 or 128 uses the workspace and
+ *                        is one launch or two, as fedattn_decode is with head_dim 128; cached rows that are not
+ *                        seen may then hold anything.
  * window >= 1, n_sink >= 0; either may exceed the lengths. */
 fedattn_status fedattn_local_window(fedattn_ctx *ctx, const fedattn_shape *shape,
                                     const void *q, const void *k, const void *v,
