@@ -70,7 +70,9 @@ constexpr uint32_t smem_bytes(int boxes)
 }
 // Keys per KV tile of an instance: weights in three bf16 parts take 3 x 16 columns of TMEM per 32 keys where S had 32; one
 // box (head_dim <= 64) has the third part beside O, whose upper 64 columns are free, two boxes have room for 64 keys only.
-__host__ __device__ constexpr int tile_keys(bool exact, int boxes) { return exact && boxes == 2 ? 64 : kTileN; }
+__host__ __device__ constexpr int tile_keys(int parts, int boxes) { return parts == 3 && boxes == 2 ? 64 : kTileN; }
+// bf16 parts of a weight
+__host__ __device__ constexpr int weight_parts(bool exact, bool window) { return !exact ? 1 : (window ? 2 : 3); }
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kColS = 0, kColO = 256;   // S (and P, aliased) of sub-tile t at kColS + 128 t; O at kColO + 128 t
 // P (bf16 pairs) of keys 64 q .. 64 q + 63 sits at S column 64 q: every 32-key chunk of P
@@ -655,7 +657,10 @@ __device__ __forceinline__ Item decode_item(const KernelParams &kp, int item, in
 //
 // kWindow: local attention through a window, with sinks.  Two key ranges per row, [lo, hi) and [0, sink), whose masks are four more bit
 // operations per word of a partial tile; tiles between the sinks and the first row's window are never loaded.  Every exponential is ex2: a
-// walk is a few tiles, and the polynomial's 7.5e-5 would be most of what lse is off by.
+// walk is a few tiles, and the polynomial's 7.5e-5 would be most of what lse is off by.  Exact instances keep two bf16 parts of a weight, 17 bits,
+// where the others keep three, which leaves room for tiles of 128 keys at two boxes: six ragged segments of 2160 tokens, 16 / 4 heads of 64,
+// window 200, 17.6 -> 15.4 us; 2 x 2048, 16 / 4 heads of 96, window 512, 50.8 -> 42.5 (windows far below a tile lose there: 5285 rows, 24 / 8
+// heads of 96, window 7, 62 -> 68).
 template <bool kSpecial, int kBoxes, bool kExact, bool kHalves, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -664,7 +669,8 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 {
     extern __shared__ uint8_t smem_raw[];
     constexpr uint32_t kTileBytes = kBoxes * kHalfBytes;                            // a Q tile
-    constexpr int kKeys = tile_keys(kExact, kBoxes), kChunks = kKeys / 32;         // keys of a KV tile, in chunks of 32
+    constexpr int kParts = weight_parts(kExact, kWindow);
+    constexpr int kKeys = tile_keys(kParts, kBoxes), kChunks = kKeys / 32;         // keys of a KV tile, in chunks of 32
     constexpr int kPartKeys = kKeys / kSplit;                                      // keys of a half of P
     constexpr uint32_t kColP3 = (kBoxes == 1 ? kColO : kColS) + 64;                // exact instances: third parts of sub-tile 0's P
     constexpr uint32_t kKvBox = kKeys * kBoxCols * 2, kKvBytes = kBoxes * kKvBox;  // a K or V tile
@@ -902,10 +908,10 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                                 const uint64_t desc = dV + (uint64_t)(st * (kKvBytes >> 4) + ks * (2048 >> 4));
                                 if (kExact) {                    // chunk of 32 keys: 16 columns each of the first, second, third parts
                                     const uint32_t a = tmem_base + kColS + t * 128 + 32 * (ks >> 1) + 8 * (ks & 1);
-                                    const uint32_t a3 = tmem_base + kColP3 + t * 128 + 16 * (ks >> 1) + 8 * (ks & 1);
                                     umma_ts(tmem_base + kColO + t * 128, a, desc, idesc_pv, (j > 0 || ks > 0));
                                     umma_ts(tmem_base + kColO + t * 128, a + 16, desc, idesc_pv, 1);
-                                    umma_ts(tmem_base + kColO + t * 128, a3, desc, idesc_pv, 1);
+                                    if (kParts == 3)
+                                        umma_ts(tmem_base + kColO + t * 128, tmem_base + kColP3 + t * 128 + 16 * (ks >> 1) + 8 * (ks & 1), desc, idesc_pv, 1);
                                 } else {
                                     umma_ts(tmem_base + kColO + t * 128, tmem_base + kColS + t * 128 + q * kPartKeys + kk * 8, desc,
                                             kIdescPV, (j > 0 || ks > 0));
@@ -1051,6 +1057,19 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         cur[2 * i + 1] = __float_as_uint(r1);
                     }
                 };
+                // Through a window two parts, each to the nearest: 2^-17 of a weight is left out, next to the output's rounding by 2^-8.
+                auto round_part = [&](bool last) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        pk[i] = pack_bf16(__uint_as_float(cur[2 * i]), __uint_as_float(cur[2 * i + 1]));
+                        if (last) continue;
+                        const uint64_t top = pack_f32x2(__uint_as_float(pk[i] << 16), __uint_as_float(pk[i] & 0xffff0000u));
+                        float r0, r1;
+                        unpack_f32x2(fma_f32x2(top, pack_f32x2(-1.f, -1.f), pack_f32x2(__uint_as_float(cur[2 * i]), __uint_as_float(cur[2 * i + 1]))), r0, r1);
+                        cur[2 * i] = __float_as_uint(r0);
+                        cur[2 * i + 1] = __float_as_uint(r1);
+                    }
+                };
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const uint64_t x2 = fma_f32x2(pack_f32x2(__uint_as_float(cur[2 * i]), __uint_as_float(cur[2 * i + 1])), sl2_2, negm2);
@@ -1068,7 +1087,12 @@ prefill_sm100_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 }
                 // keys 32 c .. 32 c + 31 as bf16 pairs: columns 64 (c / 2) + 16 (c % 2) .., all inside S columns
                 // that this thread has already read
-                if (kExact) {
+                if (kParts == 2) {
+                    round_part(false);
+                    FEDATTN_TMEM_ST16(tS + 32 * c, pk);
+                    round_part(true);
+                    FEDATTN_TMEM_ST16(tS + 32 * c + 16, pk);
+                } else if (kExact) {
                     take_part(false);
                     FEDATTN_TMEM_ST16(tS + 32 * c, pk);
                     take_part(false);
@@ -1731,8 +1755,8 @@ cudaError_t launch_prefill_sm100(Context *ctx, const PrefillParams &p, cudaStrea
     const int boxes = p.d <= kBoxCols ? 1 : 2;
     CUtensorMap mq, mk, mv, mo;
     if (!encode_map(ctx, &mq, p.q, p.n_q_rows, p.hq, p.d, false) ||
-        !encode_map(ctx, &mk, p.k, p.total_kv, p.hkv, p.d, p.kv_head_major != 0, tile_keys(p.d < 128, boxes)) ||
-        !encode_map(ctx, &mv, p.v, p.total_kv, p.hkv, p.d, p.kv_head_major != 0, tile_keys(p.d < 128, boxes)))
+        !encode_map(ctx, &mk, p.k, p.total_kv, p.hkv, p.d, p.kv_head_major != 0, tile_keys(weight_parts(p.d < 128, p.window > 0), boxes)) ||
+        !encode_map(ctx, &mv, p.v, p.total_kv, p.hkv, p.d, p.kv_head_major != 0, tile_keys(weight_parts(p.d < 128, p.window > 0), boxes)))
         return cudaErrorInvalidValue;
     // the output as [rows, heads, head_dim] in boxes of 32 rows x 64 columns; a base the encoder refuses (alignment)
     // leaves the kernel on its direct stores

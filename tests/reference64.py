@@ -88,11 +88,11 @@ def check_attention(o, lse, ref, dtype: str, what="", weights=None):
     """weights: the type that the softmax weights are stored in, where that is not the storage type.  Bounds by arithmetic.  A logit is a sum of fp32 products whose partial sums are rounded, or cut off by the tensor core, to 24
     bits, at most 2^-23 each over 8 + 2 steps, of the sum of magnitudes; the factor log2(e) and the subtraction of the reference add
     2 roundings of the logit: e_s = 2^-19 * terms.  A weight is off by e_s, by the exponential's 2^-21 and, where it is stored in
-    bf16, by 2^-8; the largest is what the row sum divides by, so both of numerator and denominator: twice that times sum p |v|.  The
+    bf16, by 2^-8 (in two bf16 parts, each to the nearest: the first leaves 2^-8, the second 2^-9 of that); the largest is what the row sum divides by, so both of numerator and denominator: twice that times sum p |v|.  The
     output is rounded by 2^-8 (bf16) or 2^-24 of itself.  Sums over keys and partials: 2^-19 of sum p |v|."""
     want_o, want_lse, weight, terms = ref
     e_s = 2.0 ** -19 * terms
-    p_err = e_s + 2.0 ** -21 + (2.0 ** -8 if (weights or dtype) == "bf16" else 0.0)
+    p_err = e_s + 2.0 ** -21 + {"bf16": 2.0 ** -8, "2 x bf16": 2.0 ** -17}.get(weights or dtype, 0.0)
     tol = (2 * p_err[..., None] + 2.0 ** -19) * weight + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(want_o) + 1e-30
     assert np.isfinite(o).all(), what
     bad = np.abs(o - want_o) > tol
