@@ -193,3 +193,44 @@ def test_two_contexts_at_once_on_two_streams():
     torch.cuda.synchronize()
     for w, o in zip(want, outs):
         assert all(torch.equal(w, x) for x in o)
+
+
+@pytest.mark.parametrize("d", [64, 96, 128])
+@pytest.mark.parametrize("cap,window", [(300, 100), (20000, 15000)])
+def test_windowed_decodes_that_feed_one_another(d, cap, window):
+    """Every output is the next call's queries, in one launch and in two: as with a synchronisation behind each call, and replayed."""
+    n, hq, hkv = 3, 8, 2
+    g = torch.Generator(device="cuda").manual_seed(d)
+    shape = fa.Shape(n, hq, hkv, d, fa.BF16)
+    ctx = fa.Context(shape, n, cap)
+    k, v = (torch.randn((cap, hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    start = torch.randn((n, hq, d), generator=g, device="cuda").bfloat16()
+    length = torch.tensor([cap], dtype=torch.int32, device="cuda")
+    x = [start.clone() for _ in range(3)]
+
+    def chain(wait):
+        for i in range(12):
+            fa.fedattn_decode_window(ctx, shape, fa.DECODE_SYNC, x[i % 3], k, v, 0, length, cap, window, 4, x[(i + 1) % 3])
+            if wait:
+                torch.cuda.synchronize()
+        return x[0].clone()
+
+    def again(run):
+        x[0].copy_(start)
+        out = run()
+        torch.cuda.synchronize()
+        return out
+
+    want = again(lambda: chain(True))
+    assert torch.equal(again(lambda: chain(False)), want)
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        chain(False)
+
+    def replay():
+        graph.replay()
+        return x[0].clone()
+
+    for _ in range(2):
+        assert torch.equal(again(replay), want)
