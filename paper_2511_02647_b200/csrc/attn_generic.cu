@@ -147,18 +147,16 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
     } else {
         kv_hi = (int)p.total_kv;
     }
-    int n_sinks = 0, gap = 0, n_keys = 0, sink_end = 0;                      // counted keys: the sinks, and how far the others are moved
+    WindowKeys keys;                                                         // (kWindow) those that the tile walks over
+    int sink_end = 0;
     if (kWindow) {
         const int len = p.mode == kLocal ? p.cu[seg + 1] - kv_lo : kv_hi, token_n = token_of(n_rows - 1);
         const bool causal = p.mode != kLocal || p.causal;
         const WindowRule first(p.mode == kLocal ? token0 : len - 1, len, p.window, p.n_sink, causal);
         const WindowRule last(p.mode == kLocal ? token_n : len - 1, len, p.window, p.n_sink, causal);
         sink_end = kv_lo + (p.n_sink < len ? p.n_sink : len);
-        n_sinks = last.sink;
-        gap = max(first.lo, n_sinks) - n_sinks;
-        n_keys = len > 0 ? n_sinks + max(0, last.hi - gap - n_sinks) : 0;
+        keys = WindowKeys(first, last, len);
     }
-    auto key_of = [&](int i) -> int { return kv_lo + i + (i >= n_sinks ? gap : 0); };      // (kWindow) the i-th of them
     const int64_t kv_base = (int64_t)kvh * p.kv_head_stride + (p.mode == kDecodeLocal ? (int64_t)seg * p.cache_stride : 0);
     const T *K = reinterpret_cast<const T *>(p.k) + kv_base, *V = reinterpret_cast<const T *>(p.v) + kv_base;
     const int32_t *kvp = p.kv_pos ? p.kv_pos + (int64_t)kvh * p.kv_pos_head_stride : nullptr;
@@ -168,22 +166,23 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
     constexpr int kVec = 16 / (int)sizeof(T), kRowVecs = kDP / kVec, kStep = kThreads / kRowVecs;
     const int ld_r = tid / kRowVecs, ld_c = (tid % kRowVecs) * kVec;
     auto load_tile = [&](T *dst, const T *src, int t) {
-        if (kWindow && t * kKeys < n_sinks) {                                // the tile where the sinks end, or one of sinks alone
+        if (kWindow && t * kKeys < keys.n_sinks) {                             // the tile where the sinks end, or one of sinks alone
             if (ld_c < d)
 #pragma unroll 1
                 for (int i = 0; i < kKeys / kStep; ++i) {
-                    const int x = t * kKeys + ld_r + i * kStep;
-                    const T *from = src + (int64_t)(x < n_keys ? key_of(x) : 0) * p.kv_tok_stride + ld_c;
+                    const int x = ld_r + i * kStep;
+                    const bool ok = x < keys.left(t, kKeys);                 // keys past the last read as zero
+                    const T *from = src + (int64_t)(ok ? kv_lo + keys.at(t * kKeys + x) : 0) * p.kv_tok_stride + ld_c;
                     const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + (ld_r + i * kStep) * L::kKvPitch + ld_c);
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(x < n_keys ? from : src), "r"(x < n_keys ? 16 : 0) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(ok ? from : src), "r"(ok ? 16 : 0) : "memory");
                 }
             asm volatile("cp.async.commit_group;" ::: "memory");
             return;
         }
         // this thread's rows: ld_r + kStep i, while below `left`
-        const int left = (kWindow ? n_keys : kv_hi - kv_lo) - t * kKeys - ld_r;
+        const int left = (kWindow ? keys.n : kv_hi - kv_lo) - t * kKeys - ld_r;
         if (ld_c < d) {                                                      // head_dim is a multiple of 8
-            const T *from = src + ((int64_t)kv_lo + (kWindow ? gap : 0) + (int64_t)t * kKeys + ld_r) * p.kv_tok_stride + ld_c;
+            const T *from = src + ((int64_t)kv_lo + (kWindow ? keys.gap : 0) + (int64_t)t * kKeys + ld_r) * p.kv_tok_stride + ld_c;
             uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + ld_r * L::kKvPitch + ld_c);
             const int64_t step = (int64_t)kStep * p.kv_tok_stride;
 #pragma unroll 4
@@ -196,7 +195,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
     };
     // the first K and V tile are on their way while Q and the rows' bounds are set up (a walk that turns out shorter
     // does not use them)
-    const int n_kt_most = kWindow ? (n_keys + kKeys - 1) / kKeys : (kv_hi > kv_lo ? (kv_hi - kv_lo - 1) / kKeys + 1 : 0);
+    const int n_kt_most = tiles_for(kWindow ? keys.n : kv_hi - kv_lo, kKeys);
     constexpr int kKvElts = L::kKvBytes / (int)sizeof(T);
     const int stages = plan.stages;
 #pragma unroll 1
@@ -272,7 +271,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
         }
     }
 
-    const int n_kt = kWindow ? n_kt_most : (kv_hi > kv_lo ? (kv_hi - kv_lo - 1) / kKeys + 1 : 0);
+    const int n_kt = kWindow ? n_kt_most : tiles_for(kv_hi - kv_lo, kKeys);
     const bool causal = p.mode != kLocal || p.causal;
     float m[kR], l[kR];
     uint64_t acc[kR / 2][kC];                                                // rows (2 i, 2 i + 1)
@@ -296,7 +295,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
 #pragma unroll
         for (int j = 0; j < kJ; ++j) {
             if (kWindow) {
-                pos[j] = key_of(min(key_l + 16 * j + t * kKeys, n_keys - 1));
+                pos[j] = kv_lo + keys.in_tile(t, kKeys, key_l + 16 * j);
                 continue;
             }
             const int key = min(key_l + 16 * j, kv_hi - 1 - kv_lo - t * kKeys) + kv_lo + t * kKeys;     // (past the end: the last one)
@@ -306,8 +305,8 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
     if (rank < n_kt) load_pos(rank);
 #pragma unroll 1
     for (int t = rank; t < n_kt; t += plan.splits) {
-        const int k0 = kWindow ? key_of(t * kKeys) : kv_lo + t * kKeys;      // the tile's first key, and keys from there to the last
-        const int left = kWindow ? n_keys - t * kKeys : kv_hi - k0;
+        const int k0 = kv_lo + (kWindow ? keys.at(t * kKeys) : t * kKeys);   // the tile's first key, and keys from there to the last
+        const int left = kWindow ? keys.left(t, kKeys) : kv_hi - k0;
         const int next = t + stages * plan.splits;                           // the tile that takes this one's place
         T *sK = sKV + 2 * slot * kKvElts, *sV = sK + kKvElts;
         slot = slot + 1 == stages ? 0 : slot + 1;
@@ -340,7 +339,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
         if (next < n_kt) load_tile(sK, K, next);
         else asm volatile("cp.async.commit_group;" ::: "memory");
         // ---- mask, online softmax (16 lanes share a row), P transposed to shared memory ----
-        const bool all_seen = !(kvp && by_pos) && !two_sided && kKeys <= left && (kWindow ? key_of(t * kKeys + kKeys - 1) <= lo_min && k0 >= wl_max : k0 + kKeys - 1 <= lo_min);
+        const bool all_seen = !(kvp && by_pos) && !two_sided && kKeys <= left && (kWindow ? kv_lo + keys.at(t * kKeys + kKeys - 1) <= lo_min && k0 >= wl_max : k0 + kKeys - 1 <= lo_min);
         float al[kR];
 #pragma unroll
         for (int i = 0; i < kR; ++i) {
@@ -392,7 +391,7 @@ attn_tiled_kernel(const __grid_constant__ GenericParams p, const __grid_constant
         const int kb = kKeyWarps > 1 ? 16 * warp : 0;
         // Through a short window most of a tile may lie behind the last key: 647 rows of 16 heads of 128 channels, window 2, 32.6 -> 29.7 us
         // (1024 rows, window 700: 168.6 -> 170.7).
-        const int kb_most = kb + (kKeyWarps > 1 ? 16 : kKeys), kb_end = kWindow ? min(kb_most, (left + 3) & ~3) : kb_most;
+        const int kb_most = kb + (kKeyWarps > 1 ? 16 : kKeys), kb_end = kWindow ? min(kb_most, (min(left, kKeys) + 3) & ~3) : kb_most;
 #pragma unroll 4
         for (int key = kb; key < kb_end; ++key) {
             uint64_t pp[kR / 2];

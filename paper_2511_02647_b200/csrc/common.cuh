@@ -8,6 +8,7 @@
 #include <string.h>
 
 #include "fedattn.h"
+#include "key_walk.cuh"
 
 namespace fedattn {
 
@@ -149,20 +150,6 @@ struct GenericParams {
     int32_t window, n_sink;       // local, decode: window > 0: see WindowRule
     int32_t n_seg;
     int32_t cu[kMaxP + 1];        // local: segment offsets
-};
-// Which keys of its segment (or cache) of `len` rows row i sees through a window: those at a distance below `window`, not behind it
-// when causal, and the first n_sink (causal: as far as they are not behind it): [lo, hi) and [0, sink).  A decode row stands at
-// len - 1 (the last cached row), causal.
-struct WindowRule {
-    int lo, hi, sink;
-    __host__ __device__ WindowRule(int i, int len, int window, int n_sink, bool causal)
-    {
-        lo = i >= window ? i - window + 1 : 0;
-        hi = causal ? i + 1 : (len - i > window ? i + window : len);
-        const int most = causal ? i + 1 : len;
-        sink = n_sink < most ? n_sink : most;
-    }
-    __device__ bool sees(int x) const { return (x >= lo && x < hi) || x < sink; }
 };
 
 // max_kv: an upper bound (decode: the caller's) on the keys of one row, which only sets how many CTAs share them
