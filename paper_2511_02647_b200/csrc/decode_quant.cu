@@ -91,23 +91,6 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 v)
     *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
 }
 
-// Which keys a cache of `len` rows shows: [0, a) and [b, len).  The walk goes over tiles of kTileKeys keys: 0 .. n_a - 1, then t_b ...
-struct Walk {
-    int a, b, len, n_a, t_b, n_tiles;
-    __device__ Walk(const QuantDecodeParams &p, int cache)
-    {
-        len = max(0, min(ld_int(p.kv_len + (p.sync ? 0 : cache)), p.max_kv_len));
-        a = len; b = len;
-        if (p.window > 0 && p.window < len) { b = len - p.window; a = min(p.n_sink, b); }
-        const int n_t = (len + kTileKeys - 1) / kTileKeys;
-        n_a = (a + kTileKeys - 1) / kTileKeys;
-        t_b = max(b / kTileKeys, n_a);
-        n_tiles = n_a + (b < len ? n_t - t_b : 0);
-    }
-    __device__ int key0(int tile) const { return (tile < n_a ? tile : t_b + (tile - n_a)) * kTileKeys; }
-    __device__ bool sees(int key) const { return key < a || (key >= b && key < len); }
-};
-
 // T: type of q and o; kD: channels; kNT: column tiles of 8 query rows; kOneLaunch: the splits are a cluster.
 template <typename T, int kD, int kNT> struct Layout {
     static constexpr int kParts = sizeof(T) == 4 ? 3 : 1;       // bf16 parts of queries and weights
@@ -159,7 +142,7 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
         raw[j].zero();
         if (i < kQWords && row < rows_here) raw[j].load(static_cast<const T *>(p.q) + out_row(chunk * kRows + row) * kD + 8 * (i - row * (kD / 8)));
     }
-    const Walk walk(p, cache);
+    const CacheWalk<kTileKeys> walk(min(ld_int(p.kv_len + (p.sync ? 0 : cache)), p.max_kv_len), p.window, p.n_sink);
     const int per = (walk.n_tiles + n_splits - 1) / n_splits;
     const int tile_lo = min(split * per, walk.n_tiles), tile_hi = min(tile_lo + per, walk.n_tiles);
     const int64_t row0 = ((int64_t)cache * p.hkv + kvh) * p.cap;
@@ -306,8 +289,7 @@ decode_quant_kernel(const __grid_constant__ QuantDecodeParams p, int n_splits, i
         }
         // ---- mask, online softmax: a row's 32 keys are 4 values in each of the 8 lanes with the same t ----
         const int key0 = walk.key0(tile);
-        const bool full = key0 + kTileKeys <= walk.a || (key0 >= walk.b && key0 + kTileKeys <= walk.len);
-        if (!full) {                                            // (-inf stays -inf under a positive factor)
+        if (!walk.sees_all(key0)) {                                         // (-inf stays -inf under a positive factor)
 #pragma unroll
             for (int mt = 0; mt < 2; ++mt)
 #pragma unroll

@@ -1,4 +1,4 @@
-// Which keys a row sees through a window, and how the tiles of a walk over them are counted.  Plain arithmetic on ints up to 2^31 - 1,
+// Which keys a row sees, through a window or in a 4-bit cache, and how the tiles of a walk over them are counted.  Plain arithmetic on ints up to 2^31 - 1,
 // for host and device: no sum here passes the last key, so none wraps where a segment or a cache is as long as an int counts.
 #pragma once
 
@@ -42,6 +42,31 @@ struct WindowKeys {
     {
         const int most = left(t, size) - 1;
         return at(t * size + (x < most ? x : most));
+    }
+};
+
+// Which keys a cache of `rows` rows shows to its new token: [0, a) and [b, len).  window 0: all of them.  The walk goes over the tiles of kKeys
+// keys 0 .. n_a - 1, then t_b and on.
+template <int kKeys> struct CacheWalk {
+    int a, b, len, n_a, t_b, n_tiles;
+    __host__ __device__ CacheWalk(int rows, int window, int n_sink)
+    {
+        len = rows > 0 ? rows : 0;
+        a = b = len;
+        if (window > 0 && window < len) { b = len - window; a = n_sink < b ? n_sink : b; }
+        const int n_t = tiles_for(len, kKeys);
+        n_a = tiles_for(a, kKeys);
+        t_b = b / kKeys > n_a ? b / kKeys : n_a;
+        n_tiles = n_a + (b < len ? n_t - t_b : 0);
+    }
+    // the first key of a tile of the walk
+    __host__ __device__ int key0(int tile) const { return (tile < n_a ? tile : t_b + (tile - n_a)) * kKeys; }
+    __host__ __device__ bool sees(int key) const { return key < a || (key >= b && key < len); }
+    // whether it sees kKeys keys from key0 on
+    __host__ __device__ bool sees_all(int key0) const 
+    {
+        const unsigned end = (unsigned)key0 + kKeys;            // up to 2^31
+        return end <= (unsigned)a || (key0 >= b && end <= (unsigned)len);
     }
 };
 

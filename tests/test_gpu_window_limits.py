@@ -1,4 +1,4 @@
-"""Windowed calls as long as an int counts: the last tile ends where 32-bit sums would wrap.  Most of the memory holds
+"""Windowed calls and 4-bit caches as long as an int counts: the last tile ends where 32-bit sums would wrap.  Most of the memory holds
 zeros; the last rows have logits that decide the output."""
 import numpy as np
 import pytest
@@ -76,3 +76,35 @@ def test_local_window_over_as_many_rows_as_an_int_counts(causal):
             y = host(x[torch.tensor(keys, device="cuda")])
             want = ref.attend(host(x[i:i + 1]), y, y, np.ones((1, len(keys)), bool), d ** -0.5)
             ref.check_attention(host(o[i:i + 1]), None, want, "bf16", "row %d" % i, "f32")
+
+
+def test_four_bit_cache_of_as_many_rows_as_an_int_counts():
+    """2^31 - 16 rows of one head of 32 channels, K and V in the same arrays (37 GB).  The last tile has 16 rows of the cache, and behind
+    the length there are some whose logits would decide everything."""
+    need(50)
+    cap, d, tail, behind = 2 ** 31 - 16, 32, 1000, 5
+    length = cap - behind
+    shape = fa.Shape(2, 1, 1, d, fa.BF16)
+    ctx = fa.Context(shape, tail, 1)
+    codes = torch.full((1, 1, cap, d // 2), 0x88, dtype=torch.uint8, device="cuda")      # zeros
+    scales = torch.zeros((1, 1, cap, 1), dtype=torch.uint8, device="cuda")
+    cache = fa.QuantCache(shape, 1, cap, codes, scales, codes, scales)
+    rng = np.random.default_rng(23)
+    x = ref.rounded(rng.standard_normal((tail, 1, d)), "bf16")
+    at = torch.arange(length - tail, length, dtype=torch.int32, device="cuda")
+    xd = dev(x.astype(np.float32), "bf16")
+    fa.fedattn_quantize_kv(ctx, shape, xd, xd, at, cache)
+    held = ref.values(*ref.quantise(x))
+    back = torch.empty_like(xd), torch.empty_like(xd)
+    fa.fedattn_dequantize_kv(ctx, shape, cache, at, *back)
+    assert ctx.poll() == 0 and all(np.array_equal(host(t), held) for t in back)
+    codes[:, :, length:], scales[:, :, length:] = 0xff, 200
+    q = ref.rounded(8.0 + rng.standard_normal((2, 1, d)), "bf16")
+    for window, sink, seen, zeros in ((0, 0, tail, length - tail), (MOST, 3, tail, length - tail), (1, MOST, tail, length - tail),
+                                      (500, 40, 500, 40)):
+        o, lse = torch.full((2, 1, d), float("nan"), dtype=torch.bfloat16, device="cuda"), torch.full((2, 1), float("nan"), device="cuda")
+        fa.fedattn_decode_quant(ctx, shape, fa.DECODE_SYNC, dev(q.astype(np.float32), "bf16"), cache,
+                                torch.tensor([length], dtype=torch.int32, device="cuda"), cap, o, lse, window, sink)
+        assert ctx.poll() == 0
+        ref.check_attention(host(o), host(lse), attend_tail(q, held[-seen:], held[-seen:], zeros, d ** -0.5), "bf16",
+                            "window %d, %d sinks" % (window, sink))

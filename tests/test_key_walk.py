@@ -1,4 +1,4 @@
-"""The walks through a window (csrc/key_walk.cuh) on the CPU: the header is compiled for the host with sums that trap when they wrap,
+"""The walks over keys (csrc/key_walk.cuh) on the CPU: the header is compiled for the host with sums that trap when they wrap,
 and compared with the definition, for short lengths key by key and for lengths up to 2^31 - 1 around every border."""
 import os
 import shutil
@@ -91,6 +91,51 @@ int main()
 }
 """
 
+CACHE = HEAD + r"""
+constexpr int kKeys = 32;
+static void check(int rows, int window, int n_sink, bool every_key)
+{
+    const CacheWalk<kKeys> w(rows, window, n_sink);
+    const ll len = std::max(rows, 0);
+    auto seen = [&](ll j) { return j >= 0 && j < len && (window == 0 || j >= len - window || j < n_sink); };
+    CHECK(w.n_tiles >= 0 && w.n_tiles <= (len + kKeys - 1) / kKeys);
+    std::vector<int> times(every_key ? len : 0);
+    std::set<int> tiles;
+    for (int t : {0, 1, w.n_a - 2, w.n_a - 1, w.n_a, w.n_a + 1, w.n_tiles - 2, w.n_tiles - 1}) tiles.insert(t);
+    if (every_key) for (int t = 0; t < w.n_tiles; ++t) tiles.insert(t);
+    for (int t : tiles) {
+        if (t < 0 || t >= w.n_tiles) continue;
+        const int k0 = w.key0(t);
+        CHECK(k0 >= 0 && k0 < len && k0 % kKeys == 0 && (t == 0 || w.key0(t - 1) < k0));
+        bool all = true;
+        for (int x = 0; x < kKeys; ++x) {
+            const ll j = (ll)k0 + x;
+            if (j <= kMost) CHECK(w.sees((int)j) == seen(j));
+            all = all && seen(j);
+            if (every_key && j < len) ++times[j];
+        }
+        CHECK(!w.sees_all(k0) || all);
+        CHECK(w.sees_all(k0) || !all || (k0 < w.a && w.a >= w.b));          // (sinks that end where the window begins may be tested)
+    }
+    for (int j = 0; j < (every_key ? len : 0); ++j) CHECK(times[j] <= 1 && (!seen(j) || times[j] == 1));
+    if (!every_key && len > 0) {                                // the ends of both ranges are in the walk's first and last tiles
+        CHECK(w.key0(w.n_tiles - 1) == (len - 1) / kKeys * kKeys);
+        if (window == 0 || window >= len) CHECK(w.n_tiles == (len - 1) / kKeys + 1);
+    }
+}
+
+int main()
+{
+    for (int rows : {-7, 0, 1, 2, 31, 32, 33, 63, 64, 100, 257})
+        for (int window : {0, 1, 2, 31, 32, 33, 100, 256, 257, 300, kMost})
+            for (int sink : {0, 1, 5, 31, 32, 33, 64, 200, 257, kMost}) check(rows, window, sink, true);
+    for (int rows : {kMost - 15, kMost - 16, kMost - 17, kMost - 20, kMost - 30, kMost - 31, kMost - 32, kMost - 33, kMost - 1000})
+        for (int window : {0, 1, 33, 1000, rows - 1, rows, kMost})
+            for (int sink : {0, 1, 40, rows - 100, rows - 1, kMost}) check(rows, window, sink, false);
+    return 0;
+}
+"""
+
 
 def run(tmp_path, text):
     if not shutil.which("g++"):
@@ -104,3 +149,7 @@ def run(tmp_path, text):
 
 def test_window_keys(tmp_path):
     run(tmp_path, WINDOW)
+
+
+def test_cache_walk(tmp_path):
+    run(tmp_path, CACHE)
