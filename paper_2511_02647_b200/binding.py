@@ -392,6 +392,12 @@ def _stream_of(ctx: Context, stream) -> int:
     return torch.cuda.current_stream(ctx.device).cuda_stream if stream is None else _stream(stream)
 
 
+def _i32(x) -> int:
+    """A number as an int32 parameter takes it, which would drop what lies above its 32 bits: beyond either end it is that end, as a count
+    more than any length, and where that is no valid value the C call refuses it."""
+    return max(-2 ** 31, min(int(x), 2 ** 31 - 1))
+
+
 def _tensor(ctx: Context, t, dtype, shape, what: str):
     """Pointer of a contiguous tensor of this type and shape on the context's device; None stays None."""
     if t is None:
@@ -421,11 +427,13 @@ def _rows(ctx: Context, t, n_rows: int, heads: int, shape: Shape, what: str):
 def _args_local_window(ctx, shape, q, k, v, cu_seqlens_host, window, n_sink, o, lse, stream):
     if len(cu_seqlens_host) != shape.n_participants + 1:
         raise ValueError("cu_seqlens must have N+1 entries")
+    if not 0 <= min(cu_seqlens_host) <= max(cu_seqlens_host) < 2 ** 31:
+        raise ValueError("cu_seqlens must be within 0 .. 2^31 - 1")
     L, hq, hkv, d, dt = int(q.shape[0]), shape.n_q_heads, shape.n_kv_heads, shape.head_dim, shape.torch_dtype
     if L != cu_seqlens_host[-1]:
         raise ValueError("q has %d rows, the segments %d" % (L, cu_seqlens_host[-1]))
     return (ctx.handle, C.byref(shape), _tensor(ctx, q, dt, (L, hq, d), "q"), _tensor(ctx, k, dt, (L, hkv, d), "k"),
-            _tensor(ctx, v, dt, (L, hkv, d), "v"), _i32_array(cu_seqlens_host), int(window), int(n_sink),
+            _tensor(ctx, v, dt, (L, hkv, d), "v"), _i32_array(cu_seqlens_host), _i32(window), _i32(n_sink),
             _tensor(ctx, o, dt, (L, hq, d), "o"), _tensor(ctx, lse, torch.float32, (L, hq), "lse"), _stream_of(ctx, stream))
 
 
@@ -451,10 +459,10 @@ def _args_decode_window(ctx, shape, mode, q, k_cache, v_cache, cache_stride_part
     held = int(max_kv_len) * row + (0 if int(mode) == DECODE_SYNC else (n - 1) * int(cache_stride_participant))
     if min(k_cache.numel(), v_cache.numel()) < held:
         raise ValueError("the caches have %d and %d elements, the call may read %d" % (k_cache.numel(), v_cache.numel(), held))
-    return (ctx.handle, C.byref(shape), int(mode), _tensor(ctx, q, dt, rows, "q"),
+    return (ctx.handle, C.byref(shape), _i32(mode), _tensor(ctx, q, dt, rows, "q"),
             *[_tensor(ctx, t, dt, t.shape, "cache") for t in (k_cache, v_cache)], int(cache_stride_participant),
-            _tensor(ctx, kv_len, torch.int32, (1 if int(mode) == DECODE_SYNC else n,), "kv_len"), int(max_kv_len), int(window),
-            int(n_sink), _tensor(ctx, o, dt, rows, "o"), _tensor(ctx, lse, torch.float32, rows[:2], "lse"),
+            _tensor(ctx, kv_len, torch.int32, (1 if int(mode) == DECODE_SYNC else n,), "kv_len"), _i32(max_kv_len), _i32(window),
+            _i32(n_sink), _tensor(ctx, o, dt, rows, "o"), _tensor(ctx, lse, torch.float32, rows[:2], "lse"),
             _stream_of(ctx, stream))
 
 
@@ -575,8 +583,8 @@ def _args_decode_quant(ctx, shape, mode, q, cache, kv_len, max_kv_len, o, lse, w
     if cache.n_caches != caches:
         raise ValueError("need %d caches, not %d" % (caches, cache.n_caches))
     rows = (n, shape.n_q_heads, shape.head_dim)
-    return (ctx.handle, C.byref(shape), int(mode), _tensor(ctx, q, shape.torch_dtype, rows, "q"), *_cache(ctx, shape, cache),
-            cache.cap_rows, _tensor(ctx, kv_len, torch.int32, (caches,), "kv_len"), int(max_kv_len), int(window), int(n_sink),
+    return (ctx.handle, C.byref(shape), _i32(mode), _tensor(ctx, q, shape.torch_dtype, rows, "q"), *_cache(ctx, shape, cache),
+            cache.cap_rows, _tensor(ctx, kv_len, torch.int32, (caches,), "kv_len"), _i32(max_kv_len), _i32(window), _i32(n_sink),
             _tensor(ctx, o, shape.torch_dtype, rows, "o"), _tensor(ctx, lse, torch.float32, rows[:2], "lse"),
             _stream_of(ctx, stream))
 
