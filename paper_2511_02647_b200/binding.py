@@ -245,12 +245,17 @@ class PreparedCall:
         # Numbers become C objects of their parameter's type here, once, and the function pointer of the call declares no types:
         # ctypes then passes everything as it is (17 arguments: 4.2 -> 2.5 us where a refused call was timed).
         args = tuple(t(a) if isinstance(a, (int, float)) else a for t, a in zip(fn.argtypes, args))
-        self._fn, self._args, self._where, self._keep = _lib._FuncPtr((where, _lib)), args, where, keep
+        self._fn, self._args, self._where, self._keep = _lib[where], args, where, keep      # (every _lib[name] is a new function object)
         self._fn.restype = C.c_int
 
     def __call__(self, stream=None):
-        # every entry point takes the stream last; `stream` (a raw cudaStream_t) replaces the prepared one
-        code = self._fn(*self._args) if stream is None else self._fn(*self._args[:-1], C.c_void_p(stream))
+        # every entry point takes the stream last; `stream` (a raw cudaStream_t as an int or a c_void_p, or an object that has one as
+        # its ctypes parameter, as torch's streams do) replaces the prepared one
+        if stream is None:
+            code = self._fn(*self._args)
+        else:
+            stream = getattr(stream, "_as_parameter_", stream)
+            code = self._fn(*self._args[:-1], stream if isinstance(stream, C.c_void_p) else C.c_void_p(stream))
         if code != 0:
             raise FedAttnError(code, self._where)
 
