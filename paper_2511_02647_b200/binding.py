@@ -562,7 +562,7 @@ def fedattn_quantize_kv(ctx: Context, shape: Shape, k, v, at, cache: QuantCache,
 
 def prepare_quantize_kv(ctx: Context, shape: Shape, k, v, at, cache: QuantCache, stream=None):
     return PreparedCall(_lib.fedattn_quantize_kv, _args_quantize_kv(ctx, shape, k, v, at, cache, stream), "fedattn_quantize_kv",
-                        (ctx, shape, k, v, at, cache))
+                        (ctx, shape, k, v, at, *cache.arrays()))
 
 
 def _args_dequantize_kv(ctx, shape, cache, at, k, v, stream):
@@ -579,7 +579,7 @@ def fedattn_dequantize_kv(ctx: Context, shape: Shape, cache: QuantCache, at, k, 
 
 def prepare_dequantize_kv(ctx: Context, shape: Shape, cache: QuantCache, at, k, v, stream=None):
     return PreparedCall(_lib.fedattn_dequantize_kv, _args_dequantize_kv(ctx, shape, cache, at, k, v, stream),
-                        "fedattn_dequantize_kv", (ctx, shape, cache, at, k, v))
+                        "fedattn_dequantize_kv", (ctx, shape, *cache.arrays(), at, k, v))
 
 
 def _args_decode_quant(ctx, shape, mode, q, cache, kv_len, max_kv_len, o, lse, window, n_sink, stream):
@@ -605,4 +605,4 @@ def prepare_decode_quant(ctx: Context, shape: Shape, mode: int, q, cache: QuantC
                          window: int = 0, n_sink: int = 0, stream=None):
     return PreparedCall(_lib.fedattn_decode_quant,
                         _args_decode_quant(ctx, shape, mode, q, cache, kv_len, max_kv_len, o, lse, window, n_sink, stream),
-                        "fedattn_decode_quant", (ctx, shape, q, cache, kv_len, o, lse))
+                        "fedattn_decode_quant", (ctx, shape, q, *cache.arrays(), kv_len, o, lse))
