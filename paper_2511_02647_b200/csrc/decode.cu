@@ -635,24 +635,26 @@ static cudaError_t launch_decode_split(const DecodeParams &p_in, int device, int
     return early_start_end(es, e != cudaSuccess ? e : cudaGetLastError());
 }
 
-static cudaError_t set_decode_smem_attr()
+// (Windowed calls apart: the attribute loads a kernel, and a program without windows need not load theirs.)
+static cudaError_t set_decode_smem_attr(bool window)
 {
     cudaError_t e = cudaSuccess;
     for (int d = 64; d <= 128; d += 32)
-        for (int i = 0; i < 8; ++i)
-            if (e == cudaSuccess && decode_stream_takes(d, i & 4))
-                e = cudaFuncSetAttribute(stream_kernel(d, 1 + (i & 1), i & 2, i & 4), cudaFuncAttributeMaxDynamicSharedMemorySize,
+        for (int i = 0; i < 4; ++i)
+            if (e == cudaSuccess && decode_stream_takes(d, window))
+                e = cudaFuncSetAttribute(stream_kernel(d, 1 + (i & 1), i & 2, window), cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          kStages * stage_bytes_of(d));
     return e;
 }
 
 cudaError_t launch_decode_bf16(const Context *ctx, const DecodeParams &p, cudaStream_t s, int64_t *launches)
 {
-    static bool attr_set[64] = {};
-    if (!attr_set[ctx->device & 63]) {
-        cudaError_t e = set_decode_smem_attr();
+    static bool attr_set[64][2] = {};
+    bool &set = attr_set[ctx->device & 63][p.window > 0];
+    if (!set) {
+        cudaError_t e = set_decode_smem_attr(p.window > 0);
         if (e != cudaSuccess) return e;
-        attr_set[ctx->device & 63] = true;
+        set = true;
     }
     return launch_decode_split(p, ctx->device, ctx->sm_count, s, launches);
 }
@@ -711,7 +713,7 @@ extern "C" fedattn_status fedattn_decode_noalloc(const fedattn_shape *shape, int
         int sms = 0;
         err = cudaGetSymbolAddress((void **)&ptr, g_decode_scratch);
         if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-        if (err == cudaSuccess) err = set_decode_smem_attr();
+        if (err == cudaSuccess) err = set_decode_smem_attr(false);
         if (err != cudaSuccess) return status_of(err);
         if (!ptr || sms < 1) return FEDATTN_ERR_CUDA;
         g_decode_sm_count[dev] = sms;
