@@ -30,15 +30,19 @@
  *   - Layouts are row-major with head_dim contiguous.  Packed queries Q[L, Hq, d]; packed keys
  *     and values K,V[L, Hkv, d]; L = sum of segment lengths; query head h reads KV head
  *     h / (Hq / Hkv).  dtype is FEDATTN_F32 or FEDATTN_BF16 for all of Q, K, V, O of a call;
- *     lse is always float.  Softmax and accumulation are fp32.
+ *     lse is always float.  Softmax and accumulation are fp32.  What the softmax weights keep in their product
+ *     with V: fp32 calls 24 bits; bf16 calls 8 at head_dim 128 and in fedattn_decode_quant (o off by 2^-8 of
+ *     sum p |v| at most, beside its own rounding), 17 in fedattn_local_window below 128, 24 in all others below 128.
+ *     lse is that of the unrounded weights.
  *   - One context serves one stream at a time: calls that share a context and may overlap on
  *     the GPU race on its workspace.
  *   - Results are those of stream order: every call behaves as if it ran after all earlier work
  *     of its stream and before all later work.  Kernels are launched with programmatic stream
  *     serialization, in two ways.  fedattn_decode (bf16, head_dim 128), fedattn_decode_window (bf16,
  *     head_dim 64, 96 or 128), fedattn_decode_noalloc, fedattn_decode_quant and the sparse modes of
- *     fedattn_aggregate_kv may touch their buffers before the preceding kernel of the stream has ended, and let the next one start before they end; the library tracks the
- *     buffers of such calls and holds a call back whenever that could be observed.  All others
+ *     fedattn_aggregate_kv may touch their buffers before the preceding kernel of the stream has ended, and let
+ *     the next one start before they end; the library tracks the buffers of such calls and holds a call
+ *     back whenever that could be observed.  All others
  *     wait for everything before them before they touch anything, and let nothing start early.
  *     Launched the ordinary way are the self-test, the kernel that prepares a bf16 head_dim 128
  *     sync call with query positions, and bf16 attention directly behind a call of the first kind.
@@ -283,7 +287,8 @@ fedattn_status fedattn_decode_noalloc(const fedattn_shape *shape, int32_t mode,
  *     elements (multiples of 8, at least Hq*d / Hkv*d; 0 = packed): rows of a joint projection are read
  *     where they lie.  q or k may be NULL, together with its output: the other is done alone.
  *   q_weight, k_weight dev [d] in shape->dtype, or NULL (ones).  eps >= 0.  A row of zeros gives zeros
- *     when eps > 0.  Squares are summed in fp32: magnitudes stay below 2^60.
+ *     when eps > 0.  Squares are summed in fp32: magnitudes stay below 2^60 and, when eps == 0, a head's largest
+ *     above 2^-50.
  *   pos dev int32 [n_rows], any value, or NULL (= row index).  inv_freq_host host double [rot_dim/2],
  *     finite, radians per position, read before the call returns (NULL when rot_dim == 0).
  *     rot_dim: multiple of 8, 0 .. d.
@@ -309,7 +314,9 @@ fedattn_status fedattn_qk_norm_rope(fedattn_ctx *ctx, const fedattn_shape *shape
  *                        caches; at dev int32 [n_rows] = cache * cap_rows + row, or NULL (= i).  A negative
  *                        entry skips the row, one beyond the caches skips it and raises FEDATTN_ERR_INDEX.
  *                        Entries that are not negative are distinct: with one row twice the caches hold
- *                        pieces of either.  Nothing but the named rows is written.
+ *                        pieces of either.  Nothing but the named rows is written.  Infinities saturate; a NaN, which
+ *                        the codes cannot say, is stored as some number and in bf16 may change the seven
+ *                        channels beside it (of the same eight) with it.
  * fedattn_dequantize_kv  the values of row at[i] to row i of k, v (dev [n_rows, Hkv, d], packed); skipped
  *                        rows keep what they hold.  For attention of many queries over such a cache: read the
  *                        rows back and call fedattn_sync. */

@@ -142,9 +142,11 @@ __device__ long long g_dtrace[1024 * 8];
 // slices, and rank r of the cluster folds and writes rows r, r + n_splits, ...
 // kWindow: the first n_sink and the last `window` keys only: the walk goes over tiles 0 .. n_a - 1, then t_b and on.  8 x 1024 of 4096 rows
 // of 8 KV heads by 32 heads, in a replayed graph: 4.8 us at 64 channels, 5.9 at 96, 5.3 at 128 (a 34 MB call; 64 and 96 channels on fp32
-// FMAs took 32 and 39); 8 queries over 30 000 shared rows 17.9, 24.8 and 22.7 (130 and 178).
+// FMAs took 32 and 39); 8 queries over 30 000 shared rows 17.9, 24.8 and 22.7 (130 and 178; the bytes take 9.4, 14.1 and 18.8).
 // kD: head_dim.  64 and 96 channels (windows only) keep their weights' 24 bits as three bf16 parts, as the fp32 weights of attn_generic.cu
-// have them, which decodes those head dims without a window; the products are not what bounds.
+// have them, which decodes those head dims without a window.  What that costs shows where 32 rows share the keys: 96 channels take longer
+// than 128 although they have three quarters of the bytes, because splitting the weights and three products on each sum, one behind
+// the other, lengthen every step of the walk.
 template <int kD, int kMTiles, bool kOneLaunch, bool kWindow>
 __global__ void __launch_bounds__(128, 2)
 decode_stream_kernel(const DecodeParams p, int n_splits, int n_chunks)

@@ -13,7 +13,9 @@
 //   * A warp has tiles of 32 keys of its own and its own ring of asynchronous copies: no barrier between warps during the walk.  Head-major
 //     rows make every copy a run of consecutive bytes.
 // The exponent reference of a row moves when its maximum has grown by more than 2^8 (one vote per tile).  fp32 queries go in as three bf16
-// parts, and so do their weights (24 bits): six products for two.
+// parts, and so do their weights (24 bits): six products for two.  bf16 calls round a weight to one bf16 behind its sum, at every head_dim: by 2^-8
+// of it at most, like the output's own rounding, where the other bf16 calls below 128 channels keep 17 or 24 bits; a second part would take
+// half as many products again in a kernel that issue slots bound.
 //
 // Up to 8 splits of a (cache, KV head) are one cluster and one launch; more are merged by a second kernel out of the workspace.
 #include <cooperative_groups.h>
